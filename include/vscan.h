@@ -341,6 +341,154 @@ int vscan_encoder_reduce_fused(const vscan_encoder_desc *desc, const void *hidde
                                void *stream);
 
 /* ---------------------------------------------------------------------------
+ * Around the pruned prefill: rotary positions of a layer's queries and keys
+ * before stage 2 (vscan_llm_prune takes them "position-encoded as the attention
+ * layer sees them"), and afterwards a paged cache of 8-bit values for the keys
+ * and values that are left ("pruned tokens never reach the cache"), written and
+ * read by every later token.
+ *
+ * vscan_rope: pair i of the leading rot_dim entries of every row (x, y) becomes
+ *   (x cos w - y sin w, x sin w + y cos w),  w = p[a(i)][b][s] * inv_freq[i],
+ * with p the position of token s of sequence b on axis a(i) (time, height,
+ * width, ...).  `inverse` turns by -w, which undoes the rotation and is the
+ * gradient of the call with respect to its input.  Entries past rot_dim are
+ * copied.  Angles are reduced in 64 bits, so far positions lose nothing; the
+ * rotation itself is in 32 bits, rounded once to `dtype`.
+ * ------------------------------------------------------------------------- */
+
+/* a(i): the sections one after the other, or pairs dealt to the axes in turn, an
+ * axis whose section is used up passed over. */
+enum { VSCAN_ROPE_SECTIONS = 0, VSCAN_ROPE_CYCLED = 1 };
+/* pair i: entries i and rot_dim/2 + i, or entries 2i and 2i + 1. */
+enum { VSCAN_ROPE_HALVES = 0, VSCAN_ROPE_ADJACENT = 1 };
+
+#define VSCAN_ROPE_MAX_AXES 4
+typedef struct {
+    uint32_t struct_size;   /* sizeof(vscan_rope_desc) */
+    int32_t dtype;          /* of q, k and the outputs */
+    int32_t batch;          /* B */
+    int32_t seq_len;        /* S tokens per sequence, >= 0 */
+    int32_t q_heads;        /* Hq, 0 .. 1024; 0: no q */
+    int32_t kv_heads;       /* Hkv, 0 .. 1024; 0: no k */
+    int32_t head_dim;       /* dh, multiple of 8, <= 256 */
+    int32_t rot_dim;        /* multiple of 8, 8 .. head_dim */
+    int32_t n_axes;         /* 1 .. 4 */
+    int32_t sections[VSCAN_ROPE_MAX_AXES]; /* pairs per axis, >= 0, rot_dim/2 in all;
+                               entries past n_axes are ignored */
+    int32_t order;          /* VSCAN_ROPE_SECTIONS / _CYCLED */
+    int32_t pairing;        /* VSCAN_ROPE_HALVES / _ADJACENT */
+    int32_t inverse;        /* 0 or 1 */
+    /* elements between sequences, heads and tokens of q and of k (entries of a row
+     * are adjacent); all three 0: contiguous [B, H, S, dh].  Multiples of 16 bytes. */
+    int64_t q_stride[3], k_stride[3];
+} vscan_rope_desc;
+
+/*
+ * q, k        DEVICE [B, Hq, S, dh], [B, Hkv, S, dh] with the strides above; NULL
+ *             where its head count is 0
+ * positions   DEVICE [n_axes, B, S] int32, any sign
+ * inv_freq    DEVICE [rot_dim/2] double: radians per position of every pair
+ * q_out,k_out DEVICE contiguous [B, H, S, dh]; NULL: that tensor is turned in
+ *             place (its strides must not let two rows share memory, or the call
+ *             is refused with VSCAN_ERR_SHAPE).  An output must not overlap an
+ *             input.
+ */
+int vscan_rope(const vscan_rope_desc *desc, void *q, void *k, const int32_t *positions,
+               const double *inv_freq, void *q_out, void *k_out, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The paged 8-bit cache.  It is made of n_blocks blocks of block_size tokens;
+ * block_table [B, max_blocks] names the blocks of every sequence, in order.  A
+ * block holds, for each kv head, e4m3 values and one fp32 scale, a power of two
+ * (value = e4m3 * scale).  With dp = head_dim rounded up to a multiple of 64:
+ *   k_cache  [n_blocks, Hkv, block_size/16, dp/16, 16 tokens, 16 dims]
+ *   v_cache  [n_blocks, Hkv, block_size/16, dp/64, 4, 16, 4, 4]: token 4*i4 + i7
+ *            of its 16, dim 64*i3 + 16*i6 + i5 (i3 .. i7: the last five indices)
+ *   k_scale, v_scale  [n_blocks, Hkv]
+ * (the order in which the matrix instructions take their operands); dims past
+ * head_dim are zero.  Nothing has to be cleared before the first use.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    uint32_t struct_size;   /* sizeof(vscan_cache_desc) */
+    int32_t dtype;          /* of q, k, v and out */
+    int32_t batch;          /* B */
+    int32_t q_heads;        /* Hq, 1 .. 1024 */
+    int32_t kv_heads;       /* Hkv, divides Hq; query head h reads kv head h/(Hq/Hkv) */
+    int32_t head_dim;       /* dh, multiple of 8, <= 256 */
+    int32_t block_size;     /* tokens per block: 16, 32, 64, 128 or 256 */
+    int32_t n_blocks;       /* blocks of the cache; n_blocks * block_size < 2^31 */
+    int32_t max_blocks;     /* row length of block_table; max_blocks * block_size < 2^31 */
+    int32_t n_new;          /* T: rows per sequence of a call (new tokens; queries) */
+    int32_t seq_len;        /* vscan_cache_store: rows between the slabs of k and v,
+                               >= n_new (0: n_new) */
+    int32_t max_len;        /* vscan_cache_attend: no sequence holds more tokens than
+                               this (longer ones are cut to it); 0: max_blocks *
+                               block_size.  A close bound makes calls faster. */
+    float scale;            /* logit scale; <= 0 selects 1/sqrt(head_dim) */
+} vscan_cache_desc;
+
+/* Bytes of k_cache (and of v_cache), and of k_scale (and of v_scale). */
+int vscan_cache_size(const vscan_cache_desc *desc, size_t *cache_bytes, size_t *scale_bytes);
+
+/* Gives the requests of a batch the blocks for their new tokens, without the host
+ * having to know a length (for instance the lengths a ragged prune leaves).
+ * Request b holds c = cached_len[b] tokens and gets n = new_len[b] more; both are
+ * held inside 0 <= c, 0 <= n <= n_new, c + n <= max_blocks * block_size.  Requests
+ * take blocks in order, from free_blocks[*free_head] on:
+ *   block_table  in/out [B, max_blocks]: entries ceil(c/block_size) ..
+ *                ceil((c+n)/block_size) - 1 of every row are written, no others
+ *   slot_map     out [B, n_new]: where row r goes, block * block_size + offset; -1
+ *                for r >= n and where the block lies outside the cache
+ *   kv_len       out [B]: c + n
+ *   free_head_out out [1]: the first entry of free_blocks not yet handed out
+ *   missing      out [1]: 0, or the number of blocks that were not there: then
+ *                nothing is handed out, block_table and the head stay as they are,
+ *                every slot is -1 and kv_len is c
+ * free_blocks is [n_free], free_head [1] (held inside 0 .. n_free).  kv_len may be
+ * cached_len, and free_head_out may be free_head; no other buffers may overlap.
+ * head_dim, heads and dtype are not used.  B <= 65535. */
+int vscan_cache_plan_workspace_size(const vscan_cache_desc *desc, size_t *bytes);
+int vscan_cache_plan(const vscan_cache_desc *desc, const int32_t *cached_len,
+                     const int32_t *new_len, const int32_t *free_blocks, int32_t n_free,
+                     const int32_t *free_head, int32_t *block_table, int32_t *slot_map,
+                     int32_t *kv_len, int32_t *free_head_out, int32_t *missing,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* Writes the keys and values of new tokens to the slots of slot_map [B, n_new] as
+ * vscan_cache_plan makes it.  k, v: [B, Hkv, n_new, dh], row r of a slab at
+ * r * dh, slabs seq_len rows apart (so the result of an in-place prune can be
+ * passed as it stands).
+ *   - A block whose offset 0 is among the new tokens is begun: its scale is the
+ *     least power of two s with |x| <= 448 s for all of them (2^-120 .. 2^120), the
+ *     values are x/s rounded to nearest even, and the rest of the block is zero.
+ *   - In a block that is continued the scale only grows: where the new tokens need
+ *     a larger one, the values before them are scaled down to it (exact, as scales
+ *     are powers of two, but for values that become subnormal).
+ * The rows of one sequence in one block have to be adjacent and in order, and no
+ * two sequences may share a block; a row whose slot does not continue its block's
+ * first one is left out, and so are slots outside the cache. */
+int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v,
+                      const int32_t *slot_map, void *k_cache, void *v_cache, float *k_scale,
+                      float *v_scale, void *stream);
+
+/* Attention of the new tokens' queries over the cache: query t of sequence b stands
+ * at position kv_len[b] - new_len[b] + t and sees the keys up to its own.
+ *   q           DEVICE [B, Hq, n_new, dh]
+ *   kv_len      DEVICE [B]: tokens in the cache, the new ones included (held inside
+ *               0 .. max_len)
+ *   new_len     DEVICE [B] (held inside 0 .. n_new), or NULL: n_new everywhere
+ *   out         DEVICE [B, Hq, n_new, dh]; rows t >= new_len[b], and rows that see
+ *               no key, are zero
+ * A block number outside the cache stands for keys that are not there.  Logits,
+ * softmax and sums are in 32 bits.  Workspace: vscan_cache_attend_workspace_size. */
+int vscan_cache_attend_workspace_size(const vscan_cache_desc *desc, size_t *bytes);
+int vscan_cache_attend(const vscan_cache_desc *desc, const void *q, const void *k_cache,
+                       const void *v_cache, const float *k_scale, const float *v_scale,
+                       const int32_t *block_table, const int32_t *kv_len,
+                       const int32_t *new_len, void *out, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
  * Host-side budget arithmetic.  Pure functions of their arguments: no GPU, no
  * state; all pointers are HOST pointers.
  * ------------------------------------------------------------------------- */

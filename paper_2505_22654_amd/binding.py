@@ -18,6 +18,9 @@ _lib = None
 VSCAN_F32, VSCAN_BF16 = 0, 1
 VSCAN_SCORE_CLS_ROW, VSCAN_SCORE_MEAN_RECEIVED = 0, 1
 VSCAN_KEYS_VISUAL_ONLY, VSCAN_KEYS_ALL = 0, 1
+VSCAN_ROPE_SECTIONS, VSCAN_ROPE_CYCLED = 0, 1
+VSCAN_ROPE_HALVES, VSCAN_ROPE_ADJACENT = 0, 1
+ROPE_MAX_AXES = 4
 (VSCAN_OK, VSCAN_ERR_NULL, VSCAN_ERR_SHAPE, VSCAN_ERR_BUDGET, VSCAN_ERR_DTYPE, VSCAN_ERR_ALIGN,
  VSCAN_ERR_WORKSPACE, VSCAN_ERR_HIP, VSCAN_ERR_VERSION, VSCAN_ERR_UNSUPPORTED) = (
     0, -1, -2, -3, -4, -5, -6, -7, -8, -9)
@@ -28,7 +31,9 @@ EXPORTS = ("vscan_encoder_workspace_size", "vscan_encoder_reduce", "vscan_llm_wo
            "vscan_llm_prune_ragged", "vscan_llm_fused_workspace_size", "vscan_llm_prune_fused",
            "vscan_encoder_fused_workspace_size", "vscan_encoder_reduce_fused",
            "vscan_llm_prune_fused_ragged", "vscan_llm_prune_static", "vscan_llm_ragged_workspace_size",
-           "vscan_llm_prune_ragged_padded", "vscan_llm_prune_fused_ragged_padded")
+           "vscan_llm_prune_ragged_padded", "vscan_llm_prune_fused_ragged_padded", "vscan_rope",
+           "vscan_cache_size", "vscan_cache_plan_workspace_size", "vscan_cache_plan", "vscan_cache_store",
+           "vscan_cache_attend_workspace_size", "vscan_cache_attend")
 STATIC_SCRATCH_BYTES = 16 << 20
 
 
@@ -52,6 +57,27 @@ class LlmDesc(ctypes.Structure):
                 ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("hidden", ctypes.c_int32), ("keep", ctypes.c_int32),
                 ("softmax_domain", ctypes.c_int32), ("in_place", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("seq_len", ctypes.c_int32),
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * ROPE_MAX_AXES),
+                ("order", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("inverse", ctypes.c_int32), ("q_stride", ctypes.c_int64 * 3),
+                ("k_stride", ctypes.c_int64 * 3)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block_size", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("n_new", ctypes.c_int32),
+                ("seq_len", ctypes.c_int32), ("max_len", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
 
 
@@ -123,6 +149,23 @@ def lib():
         L.vscan_llm_prune_fused_ragged_padded.argtypes = [ctypes.POINTER(LlmDesc), vp, vp, vp, vp,
                                                           i32p, vp, f32p, vp, ctypes.c_size_t, vp]
         L.vscan_llm_prune_fused_ragged_padded.restype = ctypes.c_int
+        L.vscan_rope.argtypes = [ctypes.POINTER(RopeDesc)] + [vp] * 7
+        L.vscan_rope.restype = ctypes.c_int
+        L.vscan_cache_size.argtypes = [ctypes.POINTER(CacheDesc)] + [ctypes.POINTER(ctypes.c_size_t)] * 2
+        L.vscan_cache_size.restype = ctypes.c_int
+        L.vscan_cache_plan_workspace_size.argtypes = [ctypes.POINTER(CacheDesc),
+                                                      ctypes.POINTER(ctypes.c_size_t)]
+        L.vscan_cache_plan_workspace_size.restype = ctypes.c_int
+        L.vscan_cache_plan.argtypes = [ctypes.POINTER(CacheDesc), vp, vp, vp, ctypes.c_int32, vp, vp, vp,
+                                       vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.vscan_cache_plan.restype = ctypes.c_int
+        L.vscan_cache_store.argtypes = [ctypes.POINTER(CacheDesc)] + [vp] * 8
+        L.vscan_cache_store.restype = ctypes.c_int
+        L.vscan_cache_attend_workspace_size.argtypes = [ctypes.POINTER(CacheDesc),
+                                                        ctypes.POINTER(ctypes.c_size_t)]
+        L.vscan_cache_attend_workspace_size.restype = ctypes.c_int
+        L.vscan_cache_attend.argtypes = [ctypes.POINTER(CacheDesc)] + [vp] * 10 + [ctypes.c_size_t, vp]
+        L.vscan_cache_attend.restype = ctypes.c_int
         L.vscan_profile_enable.argtypes = [ctypes.c_int]
         L.vscan_profile_enable.restype = ctypes.c_int
         L.vscan_profile_read.argtypes = [ctypes.POINTER(KernelTime), ctypes.c_int,
@@ -504,3 +547,254 @@ def llm_prune_fused_ragged(shape, meta, hidden, w_q, w_k_t, want_scores: bool = 
     out["out_len"] = [m[0] - m[2] + m[3] for m in meta]
     out["meta_device"], out["workspace"] = table, workspace  # alive until the work has run
     return out
+
+
+# ---- around the pruned prefill: rotary positions and the paged 8-bit cache -----------------------
+def _check(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _check_tensors(device, **tensors) -> None:
+    """Every tensor (None is passed over) on `device`, contiguous, of its dtype and shape."""
+    for name, (t, dtype, shape) in tensors.items():
+        if t is not None and not (t.device == device and t.dtype == dtype and t.is_contiguous()
+                                  and tuple(t.shape) == shape):
+            raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {device}, got {t.dtype} "
+                             f"{tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
+
+
+def _workspace(workspace, need: int, device):
+    """The caller's workspace as it is, or a new one."""
+    import torch
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    _check(workspace.device == device and workspace.dtype == torch.uint8 and workspace.is_contiguous(),
+           f"workspace: expected contiguous uint8 on {device}")
+    return workspace
+
+
+class _on_device:
+    """Makes the tensors' device the current one for a call (and yields its current stream)."""
+
+    def __init__(self, device):
+        import torch
+        self.device = device
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        import torch
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def rope_desc(shape, q_stride=(0, 0, 0), k_stride=(0, 0, 0)) -> RopeDesc:
+    """Descriptor from a `RopeShape`-like object."""
+    n = len(shape.sections)
+    _check(1 <= n <= ROPE_MAX_AXES, f"sections: 1 to {ROPE_MAX_AXES} axes, got {n}")
+    sections = (ctypes.c_int32 * ROPE_MAX_AXES)(*shape.sections)
+    return RopeDesc(ctypes.sizeof(RopeDesc), _dtype_code(shape.dtype), shape.batch, shape.seq_len,
+                    shape.q_heads, shape.kv_heads, shape.head_dim, shape.rot_dim, n, sections,
+                    shape.order, shape.pairing, shape.inverse, (ctypes.c_int64 * 3)(*q_stride),
+                    (ctypes.c_int64 * 3)(*k_stride))
+
+
+def rope_frequencies(rot_dim: int, theta: float = 10000.0, device="cuda"):
+    """Radians per position of the rot_dim/2 pairs, theta^(-2i/rot_dim), in 64 bits."""
+    import torch
+    i = torch.arange(rot_dim // 2, dtype=torch.float64, device=device)
+    return torch.pow(torch.tensor(float(theta), dtype=torch.float64, device=device), -2.0 * i / rot_dim)
+
+
+def rope(shape, positions, inv_freq, q=None, k=None, in_place: bool = False,
+         out=None) -> Dict[str, object]:
+    """vscan_rope on CUDA tensors q [B,Hq,S,dh], k [B,Hkv,S,dh] (None where the head count is 0), of any
+    strides over sequences, heads and tokens (multiples of 16 bytes), positions [axes,B,S] int32 and
+    inv_freq [rot_dim/2] float64.
+
+    Returns q and k turned: new contiguous tensors, those of `out`, or (`in_place`) the inputs."""
+    import torch
+    dt, B, S = _torch_dtype(shape.dtype), shape.batch, shape.seq_len
+    dev, dst, strides = positions.device, {}, {}
+    _check(dev.type == "cuda", "positions: expected a CUDA tensor")
+    _check_tensors(dev, positions=(positions, torch.int32, (len(shape.sections), B, S)),
+                   inv_freq=(inv_freq, torch.float64, (shape.rot_dim // 2,)))
+    for name, t, heads in (("q", q, shape.q_heads), ("k", k, shape.kv_heads)):
+        strides[name] = (0, 0, 0)
+        if heads == 0:
+            _check(t is None, f"{name}: the shape has no heads for it")
+            continue
+        size = (B, heads, S, shape.head_dim)
+        _check(t is not None and t.device == dev and t.dtype == dt and tuple(t.shape) == size,
+               f"{name}: expected {dt} {size} on {dev}")
+        if not t.is_contiguous():
+            _check(t.stride(3) == 1, f"{name}: the entries of a row must be adjacent")
+            strides[name] = t.stride()[:3]
+            if not any(strides[name]):  # one row for all: a contiguous tensor is not meant
+                t = t.contiguous()
+                strides[name] = (0, 0, 0)
+                _check(not in_place, f"{name}: rows share memory")
+        if in_place:
+            dst[name] = t
+        else:
+            dst[name] = (out or {}).get(name)
+            if dst[name] is None:
+                dst[name] = torch.empty(size, dtype=dt, device=dev)
+            _check_tensors(dev, **{f"out[{name!r}]": (dst[name], dt, size)})
+        if name == "q":
+            q = t
+        else:
+            k = t
+    desc = rope_desc(shape, strides["q"], strides["k"])
+    outs = (None, None) if in_place else (_ptr(dst.get("q")), _ptr(dst.get("k")))
+    with _on_device(dev) as stream:
+        rc = lib().vscan_rope(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq), *outs,
+                              stream)
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_rope")
+    return dst
+
+
+def cache_desc(shape, seq_len: int = 0) -> CacheDesc:
+    """Descriptor from a `CacheShape`-like object."""
+    return CacheDesc(ctypes.sizeof(CacheDesc), _dtype_code(shape.dtype), shape.batch, shape.q_heads,
+                     shape.kv_heads, shape.head_dim, shape.block_size, shape.n_blocks, shape.max_blocks,
+                     shape.n_new, seq_len, shape.max_len, shape.scale)
+
+
+def _cache_shapes(shape):
+    """(name, dtype name, tensor shape) of the parts of a cache."""
+    groups, dp = shape.block_size // 16, (shape.head_dim + 63) // 64 * 64
+    at = (shape.n_blocks, shape.kv_heads)
+    return (("k", "uint8", at + (groups, dp // 16, 16, 16)),
+            ("v", "uint8", at + (groups, dp // 64, 4, 16, 4, 4)),
+            ("k_scale", "float32", at), ("v_scale", "float32", at))
+
+
+def cache_alloc(shape, device="cuda") -> Dict[str, object]:
+    """Memory of a cache: k, v (uint8, e4m3 values in operand order) and k_scale, v_scale (fp32)."""
+    import torch
+    nc, ns = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    rc = lib().vscan_cache_size(ctypes.byref(cache_desc(shape)), ctypes.byref(nc), ctypes.byref(ns))
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_cache_size")
+    cache = {n: torch.empty(s, dtype=getattr(torch, d), device=device) for n, d, s in _cache_shapes(shape)}
+    assert cache["k"].numel() == cache["v"].numel() == nc.value
+    assert 4 * cache["k_scale"].numel() == 4 * cache["v_scale"].numel() == ns.value
+    return cache
+
+
+def _check_cache(shape, cache, device) -> None:
+    import torch
+    _check_tensors(device, **{f"cache[{n!r}]": (cache[n], getattr(torch, d), s)
+                              for n, d, s in _cache_shapes(shape)})
+
+
+def cache_plan_workspace_size(desc: CacheDesc) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().vscan_cache_plan_workspace_size(ctypes.byref(desc), ctypes.byref(n))
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_cache_plan_workspace_size")
+    return int(n.value)
+
+
+def cache_plan(shape, cached_len, new_len, free_blocks, free_head, block_table, workspace=None,
+               out=None) -> Dict[str, object]:
+    """vscan_cache_plan on int32 CUDA tensors cached_len, new_len [B], free_blocks [n_free], free_head
+    [1] and block_table [B,max_blocks] (written in place).
+
+    Returns slot_map [B,n_new], kv_len [B], free_head and missing [1], and block_table.  `out` may hold
+    any of the results; its kv_len may be cached_len and its free_head the one passed."""
+    import torch
+    i32, dev, B = torch.int32, block_table.device, shape.batch
+    desc = cache_desc(shape)
+    need = cache_plan_workspace_size(desc)
+    _check(dev.type == "cuda", "block_table: expected a CUDA tensor")
+    out = dict(out) if out else {}
+    for name, size in (("slot_map", (B, shape.n_new)), ("kv_len", (B,)), ("free_head", (1,)), ("missing", (1,))):
+        if name not in out:
+            out[name] = torch.empty(size, dtype=i32, device=dev)
+    _check_tensors(dev, cached_len=(cached_len, i32, (B,)), new_len=(new_len, i32, (B,)),
+                   free_blocks=(free_blocks, i32, (free_blocks.numel(),)), free_head=(free_head, i32, (1,)),
+                   block_table=(block_table, i32, (B, shape.max_blocks)),
+                   slot_map=(out["slot_map"], i32, (B, shape.n_new)), kv_len=(out["kv_len"], i32, (B,)),
+                   free_head_out=(out["free_head"], i32, (1,)), missing=(out["missing"], i32, (1,)))
+    workspace = _workspace(workspace, need, dev)
+    with _on_device(dev) as stream:
+        rc = lib().vscan_cache_plan(ctypes.byref(desc), _ptr(cached_len), _ptr(new_len), _ptr(free_blocks),
+                                    free_blocks.numel(), _ptr(free_head), _ptr(block_table),
+                                    _ptr(out["slot_map"]), _ptr(out["kv_len"]), _ptr(out["free_head"]),
+                                    _ptr(out["missing"]), _ptr(workspace), workspace.numel(), stream)
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_cache_plan")
+    out["block_table"], out["workspace"] = block_table, workspace
+    return out
+
+
+def cache_store(shape, k, v, slot_map, cache) -> Dict[str, object]:
+    """vscan_cache_store on CUDA tensors k, v [B,Hkv,n_new,dh], slot_map [B,n_new] int32 and a cache of
+    `cache_alloc`, which is written in place and returned.  k and v may be the first n_new rows of longer
+    slabs (what an in-place prune returns)."""
+    import torch
+    dt, dev, T, dh = _torch_dtype(shape.dtype), slot_map.device, shape.n_new, shape.head_dim
+    size, rows = (shape.batch, shape.kv_heads, T, dh), T
+    _check(dev.type == "cuda", "slot_map: expected a CUDA tensor")
+    for name, t in (("k", k), ("v", v)):
+        _check(t.device == dev and t.dtype == dt and tuple(t.shape) == size, f"{name}: expected {dt} {size} on {dev}")
+    if not (k.is_contiguous() and v.is_contiguous()):
+        _check(k.stride() == v.stride() and k.stride(3) == 1 and k.stride(2) == dh and k.stride(1) % dh == 0
+               and k.stride(1) >= T * dh
+               and (shape.batch == 1 or k.stride(0) == shape.kv_heads * k.stride(1)),
+               f"k, v: expected rows of equal slabs, got strides {k.stride()} and {v.stride()}")
+        rows = k.stride(1) // dh
+    _check_tensors(dev, slot_map=(slot_map, torch.int32, (shape.batch, T)))
+    _check_cache(shape, cache, dev)
+    desc = cache_desc(shape, rows)
+    with _on_device(dev) as stream:
+        rc = lib().vscan_cache_store(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(slot_map), _ptr(cache["k"]),
+                                     _ptr(cache["v"]), _ptr(cache["k_scale"]), _ptr(cache["v_scale"]), stream)
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_cache_store")
+    return cache
+
+
+def cache_attend_workspace_size(desc: CacheDesc) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().vscan_cache_attend_workspace_size(ctypes.byref(desc), ctypes.byref(n))
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_cache_attend_workspace_size")
+    return int(n.value)
+
+
+def cache_attend(shape, q, cache, block_table, kv_len, new_len=None, workspace=None,
+                 out=None) -> Dict[str, object]:
+    """vscan_cache_attend on CUDA tensors q [B,Hq,n_new,dh], a cache of `cache_alloc`, block_table
+    [B,max_blocks], kv_len [B] and new_len [B] int32 (None: n_new everywhere).
+
+    Returns out [B,Hq,n_new,dh] and the workspace; both may be passed in."""
+    import torch
+    i32, dt, dev, B = torch.int32, _torch_dtype(shape.dtype), q.device, shape.batch
+    desc = cache_desc(shape)
+    need = cache_attend_workspace_size(desc)
+    size = (B, shape.q_heads, shape.n_new, shape.head_dim)
+    _check(dev.type == "cuda", "q: expected a CUDA tensor")
+    workspace = _workspace(workspace, need, dev)
+    res = (out or {}).get("out")
+    if res is None:
+        res = torch.empty(size, dtype=dt, device=dev)
+    _check_tensors(dev, q=(q, dt, size), block_table=(block_table, i32, (B, shape.max_blocks)),
+                   kv_len=(kv_len, i32, (B,)), new_len=(new_len, i32, (B,)), out=(res, dt, size))
+    _check_cache(shape, cache, dev)
+    with _on_device(dev) as stream:
+        rc = lib().vscan_cache_attend(ctypes.byref(desc), _ptr(q), _ptr(cache["k"]), _ptr(cache["v"]),
+                                      _ptr(cache["k_scale"]), _ptr(cache["v_scale"]), _ptr(block_table),
+                                      _ptr(kv_len), _ptr(new_len), _ptr(res), _ptr(workspace),
+                                      workspace.numel(), stream)
+    if rc != VSCAN_OK:
+        raise VscanError(rc, "vscan_cache_attend")
+    return {"out": res, "workspace": workspace}

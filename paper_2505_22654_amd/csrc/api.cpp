@@ -340,6 +340,19 @@ struct ProfScope {
         logf("enqueued %s", name);                                                \
     } while (0)
 
+}  // namespace
+
+namespace vscan {
+// One launch of an entry point of another file, timed and logged like those of this one.
+int enqueue(const char *name, hipStream_t s, hipError_t (*launch)(const void *args, hipStream_t s),
+            const void *args) {
+    VSCAN_LAUNCH(name, launch(args, s));
+    return VSCAN_OK;
+}
+}  // namespace vscan
+
+namespace {
+
 // The score chain: part[seq][token] = sum over the query rows of their softmax weights, or with
 // `keep_rows` those weights, c_l[seq][row][token].
 int enqueue_fused_scores(FusedArgs &fa, const FusedScratch &f, unsigned char *ws, hipStream_t s) {

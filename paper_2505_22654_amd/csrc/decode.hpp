@@ -1,0 +1,90 @@
+// Launch interface of the operators around the pruned prefill: rotary positions, the paged 8-bit
+// cache and the attention over it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace vscan {
+
+// One launch of an entry point, timed and logged like the others (api.cpp).
+int enqueue(const char *name, hipStream_t s, hipError_t (*launch)(const void *args, hipStream_t s),
+            const void *args);
+
+constexpr int kRopeMaxPairs = 128;
+struct RopeArgs {
+    const void *in[2];             // q, k
+    void *out[2];
+    int64_t in_stride[2][3];       // elements: sequence, head, token
+    int64_t out_stride[2][3];
+    int heads[2];
+    const int32_t *positions;      // [axes, B, S]
+    const double *inv_freq;        // [rot/2]
+    int B, S, dh, rot, adjacent, inverse, copy_rest, is_bf16;
+    uint8_t axis[kRopeMaxPairs];   // of every pair
+};
+hipError_t launch_rope(const void *args, hipStream_t s);
+
+// head_dim rounded up to what a 16-byte load per lane of four 16-lane rows covers
+inline int cache_dp(int head_dim) { return (head_dim + 63) / 64 * 64; }
+constexpr int kCacheGroup = 16;    // tokens of a group: the rows of one matrix operand
+constexpr int kScaleExpMin = -120, kScaleExpMax = 120;
+
+struct PlanArgs {
+    const int32_t *cached_len, *new_len, *free_blocks, *free_head;
+    int32_t *block_table, *slot_map, *kv_len, *free_head_out, *missing;
+    int32_t *requests;             // scratch [B, 4]: c, n, first free entry, unused
+    int B, n_new, block_shift, n_blocks, max_blocks, n_free;
+};
+// One workgroup reads the lengths and hands the blocks out; with few rows it writes the tables too.
+inline bool plan_in_one(const PlanArgs &a) { return (int64_t)a.B * a.n_new <= 4096; }
+hipError_t launch_cache_plan(const void *args, hipStream_t s);
+hipError_t launch_cache_tables(const void *args, hipStream_t s);
+
+struct StoreArgs {
+    const void *x[2];              // k, v
+    uint8_t *cache[2];
+    float *scale[2];
+    const int32_t *slot_map;
+    int B, Hkv, n_new, seq_len, dh, block_shift, n_blocks, is_bf16;
+};
+hipError_t launch_cache_store(const void *args, hipStream_t s);
+
+struct AttendArgs {
+    const void *q;
+    const uint8_t *k_cache, *v_cache;
+    const float *k_scale, *v_scale;
+    const int32_t *block_table, *kv_len, *new_len;  // new_len may be NULL
+    void *out;
+    float *part_acc;               // [B*Hkv, rows, chunks, dp], chunks > 1 only
+    float *part_stat;              // [B*Hkv, rows, chunks, 2]: maximum, sum
+    int B, Hq, Hkv, T, dh, block_shift, n_blocks, max_blocks, max_len, is_bf16;
+    float scale;                   // times log2(e)
+    int row_tiles, split_rows;     // attend_form
+    int row_blocks, chunk, chunks;
+};
+constexpr int kAttendTile = 64;    // keys a wave takes at a time
+constexpr int kAttendWaves = 4;
+// How a call is cut into workgroups: fills the last five fields from the others.
+inline void attend_form(AttendArgs &a) {
+    const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
+    const int most = a.is_bf16 ? (a.dh > 128 ? 2 : 4) : (a.dh > 128 ? 1 : 2);
+    a.row_tiles = rows <= 16 ? 1 : rows <= 32 || most < 4 ? (most < 2 ? 1 : 2) : 4;
+    a.split_rows = rows > (int64_t)kCacheGroup * a.row_tiles;
+    const int block = kCacheGroup * a.row_tiles * (a.split_rows ? kAttendWaves : 1);
+    a.row_blocks = (int)((rows + block - 1) / block);
+    const int64_t units = (int64_t)a.B * a.Hkv * a.row_blocks;
+    const int step = kAttendTile * (a.split_rows ? 1 : kAttendWaves);
+    int64_t chunks = (1024 + units - 1) / units;
+    const int64_t most_chunks = (a.max_len + step - 1) / step;
+    if (chunks > most_chunks) chunks = most_chunks;
+    if (chunks < 1) chunks = 1;
+    const int64_t per = ((a.max_len + chunks - 1) / chunks + step - 1) / step * step;
+    a.chunk = (int)(per < step ? step : per);
+    a.chunks = (int)((a.max_len + a.chunk - 1) / a.chunk);
+    if (a.chunks < 1) a.chunks = 1;
+}
+hipError_t launch_cache_attend(const void *args, hipStream_t s);
+hipError_t launch_cache_combine(const void *args, hipStream_t s);
+
+}  // namespace vscan

@@ -127,6 +127,38 @@ class LlmShape:
 
 
 @dataclass(frozen=True)
+class RopeShape:
+    """Shape of one `vscan_rope` call."""
+    dtype: str
+    batch: int
+    seq_len: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+    rot_dim: int
+    sections: tuple          # pairs per axis, rot_dim / 2 in all
+    order: int = 0           # 0: the sections one after the other, 1: dealt to the axes in turn
+    pairing: int = 0         # 0: entries i and rot_dim/2 + i, 1: entries 2i and 2i + 1
+    inverse: int = 0
+
+
+@dataclass(frozen=True)
+class CacheShape:
+    """Shape of the `vscan_cache_*` calls of one cache."""
+    dtype: str
+    batch: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+    block_size: int          # 16, 32, 64, 128 or 256 tokens
+    n_blocks: int
+    max_blocks: int          # blocks per sequence
+    n_new: int = 1           # rows per sequence of a call
+    max_len: int = 0         # no sequence holds more tokens; 0: max_blocks * block_size
+    scale: float = 0.0       # <= 0: 1/sqrt(head_dim)
+
+
+@dataclass(frozen=True)
 class Workload:
     name: str
     seed: int

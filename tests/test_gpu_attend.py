@@ -1,0 +1,184 @@
+"""vscan_cache_attend against softmax attention in 64 bits over the values the cache holds.  Tolerance:
+`decode_reference.attend` derives it; half a step of the result's type is added for its rounding."""
+import dataclasses
+
+import numpy as np
+import pytest
+
+from paper_2505_22654_amd import binding as vb
+from paper_2505_22654_amd import workloads as wl
+from tests import decode_reference as ref
+
+pytestmark = pytest.mark.gpu
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def make(shape, lens, seed, gain=1.0, spread=3):
+    """q, a cache whose blocks hold N(0, 1) values of several scales, and a table.  Everything that no
+    token fills holds NaN: blocks nobody has, rows behind the last token, and scales of unused blocks."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    bs, dh = shape.block_size, shape.head_dim
+    dp = (dh + 63) // 64 * 64
+    cache = vb.cache_alloc(shape)
+    order = np.random.default_rng(seed).permutation(shape.n_blocks)
+    table, at = np.full((shape.batch, shape.max_blocks), -1), 0
+    tokens = torch.zeros(shape.n_blocks, dtype=torch.long)
+    for b, n in enumerate(lens):
+        k = -(-n // bs)
+        table[b, :k] = order[at:at + k]
+        for i in range(k):
+            tokens[order[at + i]] = min(bs, n - i * bs)
+        at += k
+    tokens = tokens.cuda()
+    rows = {}
+    for n in ("k", "v"):
+        e = torch.randint(-7 - spread, -6, (shape.n_blocks, shape.kv_heads), generator=g, device="cuda")
+        scale = torch.exp2(e.double())
+        x = torch.randn((shape.n_blocks, shape.kv_heads, bs, dp), generator=g, device="cuda").double() * 2.0 ** 7
+        x[..., dh:] = 0
+        values = ref.e4m3_round(x.clamp(-448, 448))
+        values = torch.where(values == 0, 0.0, values)
+        codes = ref.codes(values, shape, n)
+        held = (torch.arange(bs, device="cuda")[None] < tokens[:, None]).double()
+        mark = ref.codes(held[:, None, :, None].expand(-1, shape.kv_heads, -1, dp).contiguous(), shape, n)
+        cache[n].copy_(torch.where(mark == 0, 0x7f, codes).view(cache[n].shape))
+        cache[n + "_scale"].copy_(torch.where(tokens[:, None] > 0, scale, float("nan")).float())
+        rows[n] = (values * scale[..., None, None])[..., :dh]
+    q = (torch.randn((shape.batch, shape.q_heads, shape.n_new, dh), generator=g, device="cuda") * gain).to(vb._torch_dtype(shape.dtype))
+    return q, cache, torch.tensor(table, dtype=torch.int32, device="cuda"), rows
+
+
+def i32(v):
+    import torch
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def check(shape, q, cache, table, rows, lens, new, **kw):
+    import torch
+    kv = i32(lens)
+    got = vb.cache_attend(shape, q, cache, table, kv, None if new is None else i32(new), **kw)["out"]
+    want, bound = ref.attend(shape, q, rows["k"], rows["v"], table, lens, new)
+    torch.cuda.synchronize()
+    over = (got.double() - want).abs() - bound - HALF_STEP[shape.dtype] * want.abs()
+    assert bool(torch.isfinite(got).all()) and float(over.max()) <= 0, (shape, float(over.max()))
+    return got, want
+
+
+def run(dtype, hq, hkv, dh, block, T, lens, new=None, seed=1, max_len=0, **kw):
+    blocks = sum(-(-n // block) for n in lens) + 3
+    shape = wl.CacheShape(dtype, len(lens), hq, hkv, dh, block, blocks, max(1, max(-(-n // block) for n in lens)), T, max_len)
+    q, cache, table, rows = make(shape, lens, seed, **kw)
+    return check(shape, q, cache, table, rows, lens, new)
+
+
+LENS = [0, 1, 2, 15, 16, 17, 63, 64, 65, 130, 255, 256, 257, 1000]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,dh,block", [(4, 4, 128, 16), (28, 4, 128, 16), (7, 1, 64, 32), (8, 2, 80, 64),
+                                            (6, 3, 8, 16), (17, 1, 72, 128), (4, 2, 192, 16), (2, 1, 256, 256),
+                                            (40, 1, 128, 16), (72, 1, 64, 16), (34, 2, 200, 32)])
+def test_single_tokens(dtype, hq, hkv, dh, block):
+    run(dtype, hq, hkv, dh, block, 1, LENS, seed=hq)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,dh,block,T", [(4, 4, 128, 16, 5), (14, 2, 128, 16, 9), (4, 1, 64, 16, 33),
+                                              (2, 2, 96, 32, 130), (8, 1, 256, 16, 40), (3, 3, 24, 64, 300)])
+def test_several_tokens_see_the_keys_up_to_their_own(dtype, hq, hkv, dh, block, T):
+    """Lengths below T leave the first queries without a key."""
+    run(dtype, hq, hkv, dh, block, T, [0, 1, T - 1, T, T + 1, 64, 333, 700], seed=T)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [4, 70])
+def test_ragged_batches(dtype, T):
+    """Padding rows are zero; new_len outside its range is held inside it."""
+    lens = [500, 33, 64, 7, 0, 1000, 100]
+    new = [T, 1, 0, T, T, T - 1, T + 9]
+    got, _ = run(dtype, 12, 4, 128, 16, T, lens, new, seed=3)
+    for b, n in enumerate(new):
+        assert not got[b, :, min(n, T):].any()
+    got, want = run(dtype, 4, 2, 64, 16, T, [90, 80], [-5, T], seed=4)
+    assert not got[0].any()
+
+
+@pytest.mark.parametrize("hq,hkv,T", [(28, 4, 1), (8, 1, 2), (4, 4, 3), (16, 1, 20)])
+def test_long_caches_in_chunks(hq, hkv, T):
+    for dtype in ("bf16", "f32"):
+        run(dtype, hq, hkv, 128, 16, T, [9000, 4100], seed=5)
+        run(dtype, hq, hkv, 64, 64, T, [20000], seed=6)
+
+
+def test_large_logits_and_scales_far_apart():
+    """Softmax that all but picks one key, references raised many times, scales 2^-37 .. 2^-7."""
+    for dtype in ("bf16", "f32"):
+        run(dtype, 8, 2, 128, 16, 3, [700, 65], gain=8.0, seed=7)
+        run(dtype, 4, 4, 64, 16, 1, [700, 65], spread=30, seed=8)
+
+
+def test_max_len_bounds_the_keys():
+    import torch
+    for T in (1, 40):
+        got, _ = run("bf16", 8, 2, 128, 16, T, [700, 300, 64, 301], max_len=301, seed=9)
+        assert torch.isfinite(got).all()
+
+
+def test_lengths_outside_the_table_are_held_inside_it():
+    shape = wl.CacheShape("bf16", 3, 4, 2, 64, 16, 20, 5, 2)
+    q, cache, table, rows = make(shape, [80, 33, 80], 3)
+    got = vb.cache_attend(shape, q, cache, table, i32([2 ** 31 - 1, -7, 81]))["out"]
+    want = vb.cache_attend(shape, q, cache, table, i32([80, 0, 80]))["out"]
+    assert bool((got == want).all()) and not got[1].any()
+
+
+@pytest.mark.parametrize("T", [1, 50])
+def test_blocks_outside_the_cache_are_not_there(T):
+    import torch
+    shape = wl.CacheShape("bf16", 3, 8, 4, 128, 16, 60, 20, T)
+    lens = [300, 320, 40]
+    q, cache, table, rows = make(shape, lens, 11)
+    table[0, 3], table[0, 18] = -1, 60
+    table[1, ::2] = 2 ** 31 - 1
+    table[2, :] = -2 ** 31
+    got, _ = check(shape, q, cache, table, rows, lens, None)
+    assert not got[2].any()
+
+
+def test_queries_zeros_give_the_mean_of_the_values():
+    import torch
+    shape = wl.CacheShape("f32", 1, 2, 1, 64, 16, 40, 33, 1)
+    q, cache, table, rows = make(shape, [517], 2)
+    got = vb.cache_attend(shape, torch.zeros_like(q), cache, table, i32([517]))["out"]
+    j = torch.arange(517, device="cuda")
+    mean = rows["v"][table[0].long()[j // 16], 0, j % 16].mean(0)
+    assert float((got.double() - mean).abs().max()) <= 1e-5 * float(rows["v"].abs().mean())
+
+
+def test_given_buffers_and_scale():
+    import torch
+    shape = wl.CacheShape("bf16", 1, 4, 4, 64, 16, 400, 400, 2, scale=0.37)
+    q, cache, table, rows = make(shape, [6000], 5)
+    ws = torch.full((vb.cache_attend_workspace_size(vb.cache_desc(shape)),), 255, dtype=torch.uint8, device="cuda")
+    out = {"out": torch.full_like(q, float("nan"))}
+    got, _ = check(shape, q, cache, table, rows, [6000], None, workspace=ws, out=out)
+    assert got is out["out"]
+    with pytest.raises(vb.VscanError):
+        vb.cache_attend(shape, q, cache, table, i32([6000]), workspace=ws[:-256])
+    with pytest.raises(ValueError):
+        vb.cache_attend(shape, q.float(), cache, table, i32([6000]))
+    with pytest.raises(ValueError):
+        vb.cache_attend(shape, q, cache, table[:, :-1], i32([6000]))
+    with pytest.raises(ValueError):
+        vb.cache_attend(shape, q, {**cache, "v": cache["k"]}, table, i32([6000]))
+
+
+def test_results_do_not_depend_on_the_run():
+    import torch
+    shape = wl.CacheShape("bf16", 4, 28, 4, 128, 16, 800, 200, 1)
+    q, cache, table, rows = make(shape, [3000, 100, 2222, 5], 12)
+    kv = i32([3000, 100, 2222, 5])
+    first = vb.cache_attend(shape, q, cache, table, kv)["out"]
+    for _ in range(3):
+        assert torch.equal(vb.cache_attend(shape, q, cache, table, kv)["out"], first)

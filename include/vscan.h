@@ -464,9 +464,11 @@ int vscan_cache_plan(const vscan_cache_desc *desc, const int32_t *cached_len,
  *   - In a block that is continued the scale only grows: where the new tokens need
  *     a larger one, the values before them are scaled down to it (exact, as scales
  *     are powers of two, but for values that become subnormal).
- * The rows of one sequence in one block have to be adjacent and in order, and no
- * two sequences may share a block; a row whose slot does not continue its block's
- * first one is left out, and so are slots outside the cache. */
+ * Row r of a sequence goes to offset (o + r) mod block_size of its block, o the
+ * offset of row 0's slot (0 where that is negative), and the rows of one block
+ * follow each other in it.  A row whose slot says otherwise, or whose block's first
+ * row here or a row between does, is left out, and so are slots outside the cache.
+ * No two sequences may share a block that is written. */
 int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v,
                       const int32_t *slot_map, void *k_cache, void *v_cache, float *k_scale,
                       float *v_scale, void *stream);
@@ -480,7 +482,8 @@ int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v
  *   out         DEVICE [B, Hq, n_new, dh]; rows t >= new_len[b], and rows that see
  *               no key, are zero
  * A block number outside the cache stands for keys that are not there.  Logits,
- * softmax and sums are in 32 bits.  Workspace: vscan_cache_attend_workspace_size. */
+ * softmax and sums are in 32 bits.  Workspace: vscan_cache_attend_workspace_size
+ * bytes, 16-byte aligned (0: none is needed, NULL is taken). */
 int vscan_cache_attend_workspace_size(const vscan_cache_desc *desc, size_t *bytes);
 int vscan_cache_attend(const vscan_cache_desc *desc, const void *q, const void *k_cache,
                        const void *v_cache, const float *k_scale, const float *v_scale,

@@ -555,42 +555,41 @@ def _check(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _check_tensors(device, **tensors) -> None:
-    """Every tensor (None is passed over) on `device`, contiguous, of its dtype and shape."""
-    for name, (t, dtype, shape) in tensors.items():
-        if t is not None and not (t.device == device and t.dtype == dtype and t.is_contiguous()
-                                  and tuple(t.shape) == shape):
-            raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {device}, got {t.dtype} "
-                             f"{tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
+def _check_tensor(name: str, t, dtype, shape, device) -> None:
+    """`t` on `device`, contiguous, of this dtype and shape."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {device}, got {t.dtype} "
+                         f"{tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
 
 
 def _workspace(workspace, need: int, device):
-    """The caller's workspace as it is, or a new one."""
+    """The caller's workspace as it is, or a new one where one is needed."""
     import torch
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _check(workspace.device == device and workspace.dtype == torch.uint8 and workspace.is_contiguous(),
            f"workspace: expected contiguous uint8 on {device}")
     return workspace
 
 
-class _on_device:
-    """Makes the tensors' device the current one for a call (and yields its current stream)."""
+def _call(entry: str, device, *args) -> None:
+    """Calls `entry` on the current stream of `device`, with that device the current one."""
+    import torch
+    fn, index = getattr(lib(), entry), device.index
+    if index == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(index))
+    if rc != VSCAN_OK:
+        raise VscanError(rc, entry)
 
-    def __init__(self, device):
-        import torch
-        self.device = device
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
-    def __enter__(self):
-        import torch
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _raw_stream(index: int) -> int:
+    """Handle of the device's current stream, without the stream object that torch.cuda.current_stream
+    makes around it (4 of the 19 us that a small call took)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def rope_desc(shape, q_stride=(0, 0, 0), k_stride=(0, 0, 0)) -> RopeDesc:
@@ -620,44 +619,35 @@ def rope(shape, positions, inv_freq, q=None, k=None, in_place: bool = False,
     Returns q and k turned: new contiguous tensors, those of `out`, or (`in_place`) the inputs."""
     import torch
     dt, B, S = _torch_dtype(shape.dtype), shape.batch, shape.seq_len
-    dev, dst, strides = positions.device, {}, {}
-    _check(dev.type == "cuda", "positions: expected a CUDA tensor")
-    _check_tensors(dev, positions=(positions, torch.int32, (len(shape.sections), B, S)),
-                   inv_freq=(inv_freq, torch.float64, (shape.rot_dim // 2,)))
-    for name, t, heads in (("q", q, shape.q_heads), ("k", k, shape.kv_heads)):
-        strides[name] = (0, 0, 0)
+    dev, src, dst, strides = positions.device, [None, None], [None, None], [(0, 0, 0), (0, 0, 0)]
+    _check(positions.is_cuda, "positions: expected a CUDA tensor")
+    _check_tensor("positions", positions, torch.int32, (len(shape.sections), B, S), dev)
+    _check_tensor("inv_freq", inv_freq, torch.float64, (shape.rot_dim // 2,), dev)
+    for i, (name, t, heads) in enumerate((("q", q, shape.q_heads), ("k", k, shape.kv_heads))):
         if heads == 0:
             _check(t is None, f"{name}: the shape has no heads for it")
             continue
         size = (B, heads, S, shape.head_dim)
-        _check(t is not None and t.device == dev and t.dtype == dt and tuple(t.shape) == size,
-               f"{name}: expected {dt} {size} on {dev}")
+        if t is None or t.dtype is not dt or t.shape != size or t.device != dev:
+            raise ValueError(f"{name}: expected {dt} {size} on {dev}")
         if not t.is_contiguous():
-            _check(t.stride(3) == 1, f"{name}: the entries of a row must be adjacent")
-            strides[name] = t.stride()[:3]
-            if not any(strides[name]):  # one row for all: a contiguous tensor is not meant
-                t = t.contiguous()
-                strides[name] = (0, 0, 0)
-                _check(not in_place, f"{name}: rows share memory")
+            *strides[i], entry = t.stride()
+            if entry != 1 or not any(strides[i]):  # three zeros would mean a contiguous tensor
+                raise ValueError(f"{name}: the entries of a row must be adjacent, and rows apart")
+        src[i] = t
         if in_place:
-            dst[name] = t
+            dst[i] = t
         else:
-            dst[name] = (out or {}).get(name)
-            if dst[name] is None:
-                dst[name] = torch.empty(size, dtype=dt, device=dev)
-            _check_tensors(dev, **{f"out[{name!r}]": (dst[name], dt, size)})
-        if name == "q":
-            q = t
-        else:
-            k = t
-    desc = rope_desc(shape, strides["q"], strides["k"])
-    outs = (None, None) if in_place else (_ptr(dst.get("q")), _ptr(dst.get("k")))
-    with _on_device(dev) as stream:
-        rc = lib().vscan_rope(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq), *outs,
-                              stream)
-    if rc != VSCAN_OK:
-        raise VscanError(rc, "vscan_rope")
-    return dst
+            dst[i] = out.get(name) if out else None
+            if dst[i] is None:
+                dst[i] = torch.empty(size, dtype=dt, device=dev)
+            else:
+                _check_tensor(f"out[{name!r}]", dst[i], dt, size, dev)
+    desc = rope_desc(shape, *strides)
+    outs = (None, None) if in_place else (_ptr(dst[0]), _ptr(dst[1]))
+    _call("vscan_rope", dev, ctypes.byref(desc), _ptr(src[0]), _ptr(src[1]), positions.data_ptr(),
+          inv_freq.data_ptr(), *outs)
+    return {n: t for n, t in zip("qk", dst) if t is not None}
 
 
 def cache_desc(shape, seq_len: int = 0) -> CacheDesc:
@@ -691,8 +681,8 @@ def cache_alloc(shape, device="cuda") -> Dict[str, object]:
 
 def _check_cache(shape, cache, device) -> None:
     import torch
-    _check_tensors(device, **{f"cache[{n!r}]": (cache[n], getattr(torch, d), s)
-                              for n, d, s in _cache_shapes(shape)})
+    for n, d, s in _cache_shapes(shape):
+        _check_tensor(n, cache[n], torch.uint8 if d == "uint8" else torch.float32, s, device)
 
 
 def cache_plan_workspace_size(desc: CacheDesc) -> int:
@@ -714,24 +704,23 @@ def cache_plan(shape, cached_len, new_len, free_blocks, free_head, block_table, 
     i32, dev, B = torch.int32, block_table.device, shape.batch
     desc = cache_desc(shape)
     need = cache_plan_workspace_size(desc)
-    _check(dev.type == "cuda", "block_table: expected a CUDA tensor")
+    _check(block_table.is_cuda, "block_table: expected a CUDA tensor")
+    _check_tensor("cached_len", cached_len, i32, (B,), dev)
+    _check_tensor("new_len", new_len, i32, (B,), dev)
+    _check_tensor("free_blocks", free_blocks, i32, (free_blocks.numel(),), dev)
+    _check_tensor("free_head", free_head, i32, (1,), dev)
+    _check_tensor("block_table", block_table, i32, (B, shape.max_blocks), dev)
     out = dict(out) if out else {}
     for name, size in (("slot_map", (B, shape.n_new)), ("kv_len", (B,)), ("free_head", (1,)), ("missing", (1,))):
-        if name not in out:
+        if name in out:
+            _check_tensor(f"out[{name!r}]", out[name], i32, size, dev)
+        else:
             out[name] = torch.empty(size, dtype=i32, device=dev)
-    _check_tensors(dev, cached_len=(cached_len, i32, (B,)), new_len=(new_len, i32, (B,)),
-                   free_blocks=(free_blocks, i32, (free_blocks.numel(),)), free_head=(free_head, i32, (1,)),
-                   block_table=(block_table, i32, (B, shape.max_blocks)),
-                   slot_map=(out["slot_map"], i32, (B, shape.n_new)), kv_len=(out["kv_len"], i32, (B,)),
-                   free_head_out=(out["free_head"], i32, (1,)), missing=(out["missing"], i32, (1,)))
     workspace = _workspace(workspace, need, dev)
-    with _on_device(dev) as stream:
-        rc = lib().vscan_cache_plan(ctypes.byref(desc), _ptr(cached_len), _ptr(new_len), _ptr(free_blocks),
-                                    free_blocks.numel(), _ptr(free_head), _ptr(block_table),
-                                    _ptr(out["slot_map"]), _ptr(out["kv_len"]), _ptr(out["free_head"]),
-                                    _ptr(out["missing"]), _ptr(workspace), workspace.numel(), stream)
-    if rc != VSCAN_OK:
-        raise VscanError(rc, "vscan_cache_plan")
+    _call("vscan_cache_plan", dev, ctypes.byref(desc), cached_len.data_ptr(), new_len.data_ptr(),
+          free_blocks.data_ptr(), free_blocks.numel(), free_head.data_ptr(), block_table.data_ptr(),
+          out["slot_map"].data_ptr(), out["kv_len"].data_ptr(), out["free_head"].data_ptr(),
+          out["missing"].data_ptr(), workspace.data_ptr(), workspace.numel())
     out["block_table"], out["workspace"] = block_table, workspace
     return out
 
@@ -743,23 +732,21 @@ def cache_store(shape, k, v, slot_map, cache) -> Dict[str, object]:
     import torch
     dt, dev, T, dh = _torch_dtype(shape.dtype), slot_map.device, shape.n_new, shape.head_dim
     size, rows = (shape.batch, shape.kv_heads, T, dh), T
-    _check(dev.type == "cuda", "slot_map: expected a CUDA tensor")
+    _check(slot_map.is_cuda, "slot_map: expected a CUDA tensor")
     for name, t in (("k", k), ("v", v)):
-        _check(t.device == dev and t.dtype == dt and tuple(t.shape) == size, f"{name}: expected {dt} {size} on {dev}")
+        if t.dtype is not dt or t.shape != size or t.device != dev:
+            raise ValueError(f"{name}: expected {dt} {size} on {dev}")
     if not (k.is_contiguous() and v.is_contiguous()):
         _check(k.stride() == v.stride() and k.stride(3) == 1 and k.stride(2) == dh and k.stride(1) % dh == 0
                and k.stride(1) >= T * dh
                and (shape.batch == 1 or k.stride(0) == shape.kv_heads * k.stride(1)),
                f"k, v: expected rows of equal slabs, got strides {k.stride()} and {v.stride()}")
         rows = k.stride(1) // dh
-    _check_tensors(dev, slot_map=(slot_map, torch.int32, (shape.batch, T)))
+    _check_tensor("slot_map", slot_map, torch.int32, (shape.batch, T), dev)
     _check_cache(shape, cache, dev)
     desc = cache_desc(shape, rows)
-    with _on_device(dev) as stream:
-        rc = lib().vscan_cache_store(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(slot_map), _ptr(cache["k"]),
-                                     _ptr(cache["v"]), _ptr(cache["k_scale"]), _ptr(cache["v_scale"]), stream)
-    if rc != VSCAN_OK:
-        raise VscanError(rc, "vscan_cache_store")
+    _call("vscan_cache_store", dev, ctypes.byref(desc), k.data_ptr(), v.data_ptr(), slot_map.data_ptr(),
+          cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr())
     return cache
 
 
@@ -782,19 +769,20 @@ def cache_attend(shape, q, cache, block_table, kv_len, new_len=None, workspace=N
     desc = cache_desc(shape)
     need = cache_attend_workspace_size(desc)
     size = (B, shape.q_heads, shape.n_new, shape.head_dim)
-    _check(dev.type == "cuda", "q: expected a CUDA tensor")
+    _check(q.is_cuda, "q: expected a CUDA tensor")
+    _check_tensor("q", q, dt, size, dev)
+    _check_tensor("block_table", block_table, i32, (B, shape.max_blocks), dev)
+    _check_tensor("kv_len", kv_len, i32, (B,), dev)
+    if new_len is not None:
+        _check_tensor("new_len", new_len, i32, (B,), dev)
+    _check_cache(shape, cache, dev)
     workspace = _workspace(workspace, need, dev)
-    res = (out or {}).get("out")
+    res = out.get("out") if out else None
     if res is None:
         res = torch.empty(size, dtype=dt, device=dev)
-    _check_tensors(dev, q=(q, dt, size), block_table=(block_table, i32, (B, shape.max_blocks)),
-                   kv_len=(kv_len, i32, (B,)), new_len=(new_len, i32, (B,)), out=(res, dt, size))
-    _check_cache(shape, cache, dev)
-    with _on_device(dev) as stream:
-        rc = lib().vscan_cache_attend(ctypes.byref(desc), _ptr(q), _ptr(cache["k"]), _ptr(cache["v"]),
-                                      _ptr(cache["k_scale"]), _ptr(cache["v_scale"]), _ptr(block_table),
-                                      _ptr(kv_len), _ptr(new_len), _ptr(res), _ptr(workspace),
-                                      workspace.numel(), stream)
-    if rc != VSCAN_OK:
-        raise VscanError(rc, "vscan_cache_attend")
+    else:
+        _check_tensor("out", res, dt, size, dev)
+    _call("vscan_cache_attend", dev, ctypes.byref(desc), q.data_ptr(), cache["k"].data_ptr(), cache["v"].data_ptr(),
+          cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
+          _ptr(new_len), res.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel())
     return {"out": res, "workspace": workspace}

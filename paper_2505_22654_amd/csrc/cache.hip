@@ -112,10 +112,12 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(PlanArgs a,
 }
 
 // ---- new keys and values -----------------------------------------------------------------------
-// One workgroup per (k or v, sequence, kv head, block that the new rows touch): the largest absolute
-// value of the block's new rows gives the scale, then every 16-byte piece of the block that changes
-// is made anew.  Bound: HBM (2 or 4 bytes in and one out per value); the rows are read twice, the
-// second time from the cache.
+// A page (a block's part of one kv head, of k or of v) is the work of one wave up to 32 tokens, of a
+// workgroup above.  A lane owns units of 4 tokens x 8 dims: it loads them with whole rows side by side,
+// and keeps them while the largest absolute value of the page's new rows gives the scale.  After
+// rounding it holds 32 bytes that belong to pieces of its neighbours: one exchange (k) or a 4x4
+// transposition (v) between lanes of a quad leaves two whole 16-byte pieces of the page per unit.
+// Bound: HBM (2 or 4 bytes in and one out per value).
 constexpr int kStoreThreads = 256;
 
 // least e with amax <= 448 * 2^e (448 = 1.75 * 2^8), held inside what a scale may be
@@ -136,41 +138,186 @@ __device__ __forceinline__ uint32_t rescale_fp8(uint32_t w, float f) {
                   __builtin_amdgcn_cvt_f32_fp8(w, 2) * f, __builtin_amdgcn_cvt_f32_fp8(w, 3) * f);
 }
 
+// the value of the lane whose number differs in bit 0 (or bit 1)
+__device__ __forceinline__ uint32_t from_xor1(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true);
+}
+__device__ __forceinline__ uint32_t from_xor2(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true);
+}
+// w[e] of lane q of a quad -> w[q] of lane e, as w[e]
+__device__ __forceinline__ void transpose4(uint32_t *w, int q) {
+    const bool o1 = q & 1, o2 = q & 2;
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+        const uint32_t r = from_xor1(o1 ? w[e] : w[e + 1]);
+        if (o1) w[e] = r;
+        else w[e + 1] = r;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t r = from_xor2(o2 ? w[e] : w[e + 2]);
+        if (o2) w[e] = r;
+        else w[e + 2] = r;
+    }
+}
+
+// A unit of a page: 4 tokens from `token` on, 8 dims from `dim` on, and where its two pieces lie.
+struct Unit {
+    int token, dim, piece[2], piece_token[2];  // bytes from the start of the page
+};
+template <int DP>
+__device__ __forceinline__ Unit unit_at(int u, int kind) {
+    const int p = u % (DP / 8), quad = u / (DP / 8), group = (quad >> 2) * kCacheGroup * DP;
+    Unit r;
+    r.token = quad * 4;
+    if (kind == 0) {  // [dp/16][16 tokens][16 dims]: lanes 2c and 2c + 1 hold the halves of column c
+        r.dim = p * 8;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r.piece_token[i] = quad * 4 + 2 * i + (p & 1);
+            r.piece[i] = group + (p >> 1) * 256 + ((quad & 3) * 4 + 2 * i + (p & 1)) * 16;
+        }
+    } else {  // [dp/64][4 quads][16 dims][4][4 tokens]: the lanes of a quad hold dims 16 apart
+        r.dim = (p >> 3) * 64 + (p & 3) * 16 + (p >> 2 & 1) * 8;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r.piece_token[i] = quad * 4;
+            r.piece[i] = group + (p >> 3) * 1024 + (quad & 3) * 256 + ((p >> 2 & 1) * 8 + 4 * i + (p & 3)) * 16;
+        }
+    }
+    return r;
+}
+
+// What a unit's rows look like in memory: 8 entries of each of 4 tokens.
 template <typename T>
-__global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(StoreArgs a, int dp, int runs) {
+struct Rows {
+    static constexpr int kLoads = 8 / ElemTraits<T>::kPer16B;
+    uint4 raw[4][kLoads];
+    __device__ __forceinline__ void load(const T *src, int row, int n, int dim, int dh) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                raw[j][i] = load16_stream_guard(src, ((int64_t)(row + j) * dh + dim) * (int)sizeof(T) + 16 * i,
+                                                row + j >= 0 && row + j < n && dim < dh);
+    }
+    __device__ __forceinline__ void get(int j, float *f) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) unpack16<T>(raw[j][i], f + i * ElemTraits<T>::kPer16B);
+    }
+    // rows from n on were read before it was known that they go elsewhere
+    __device__ __forceinline__ float largest(int row, int n) const {
+        float m = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float f[8], r = 0.f;
+            get(j, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r = fmaxf(r, fabsf(f[e]));
+            m = row + j < n ? fmaxf(m, r) : m;
+        }
+        return m;
+    }
+    // the unit's two pieces
+    __device__ __forceinline__ void pieces(int kind, float inv, uint4 *out) const {
+        if (kind == 0) {
+            uint32_t w[4][2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float f[8];
+                get(j, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] *= inv;
+                w[j][0] = to_fp8(f[0], f[1], f[2], f[3]);
+                w[j][1] = to_fp8(f[4], f[5], f[6], f[7]);
+            }
+            const bool odd = lane_id() & 1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {  // even lanes keep tokens 0 and 2, odd ones 1 and 3
+                const uint32_t *mine = odd ? w[2 * i + 1] : w[2 * i], *theirs = odd ? w[2 * i] : w[2 * i + 1];
+                const uint32_t a = mine[0], b = mine[1];
+                const uint32_t c = from_xor1(theirs[0]), d = from_xor1(theirs[1]);
+                out[i] = odd ? make_uint4(c, d, a, b) : make_uint4(a, b, c, d);
+            }
+        } else {
+            float f[4][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) get(j, f[j]);
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = to_fp8(f[0][e] * inv, f[1][e] * inv, f[2][e] * inv, f[3][e] * inv);
+            transpose4(w, lane_id() & 3);
+            transpose4(w + 4, lane_id() & 3);
+            out[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            out[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+};
+
+// kHold: units that a lane keeps between the two passes; further ones are read again.
+template <typename T, int DP, int LANES, int kHold>
+__global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(StoreArgs a, int runs, int pages) {
     __shared__ float red[kStoreThreads / kWave];
     __shared__ int first_bad;
-    const int kind = blockIdx.y;
-    const int run = blockIdx.x % runs, hk = blockIdx.x / runs % a.Hkv, b = blockIdx.x / runs / a.Hkv;
+    const int lane = threadIdx.x % LANES;
+    int id = blockIdx.x * (kStoreThreads / LANES) + (LANES == kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0);
+    if (id >= pages) return;
+    const int kind = id % 2;
+    id /= 2;
+    const int run = id % runs, hk = id / runs % a.Hkv, b = id / runs / a.Hkv;
     const int size = 1 << a.block_shift;
     const int32_t *slots = a.slot_map + (int64_t)b * a.n_new;
     const int s0 = slots[0];
     const int off0 = s0 >= 0 ? s0 & (size - 1) : 0;
     const int r0 = max(0, run * size - off0), r1 = min(a.n_new, (run + 1) * size - off0);
     if (r0 >= r1) return;
-    const int slot = slots[r0];
-    if (slot < 0 || (slot >> a.block_shift) >= a.n_blocks) return;
-    const int64_t page = (int64_t)(slot >> a.block_shift) * a.Hkv + hk;
-    const int off = slot & (size - 1);
-    // rows that continue the first one inside its block
-    if (threadIdx.x == 0) first_bad = min(r1 - r0, size - off);
-    __syncthreads();
-    for (int i = threadIdx.x; i < r1 - r0; i += kStoreThreads)
-        if (slots[r0 + i] != slot + i) atomicMin(&first_bad, i);
-    __syncthreads();
-    const int n = first_bad;
-
+    // the run's rows start at this offset wherever they go (off below, for slots as they are made)
+    const int at0 = run ? 0 : off0;
     const T *src = static_cast<const T *>(a.x[kind]) + ((int64_t)(b * a.Hkv + hk) * a.seq_len + r0) * a.dh;
-    constexpr int kPer = ElemTraits<T>::kPer16B;
-    float amax = 0.f;
-    for (int i = threadIdx.x; i < n * a.dh / kPer; i += kStoreThreads) {
-        float f[kPer];
-        unpack16<T>(load16(src, (int64_t)i * 16), f);
+    const int q0 = at0 / 4, q1 = (at0 + r1 - r0 + 3) / 4;  // quads of tokens that the rows lie in
+    const int units = (q1 - q0) * (DP / 8);
+    Rows<T> held[kHold];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) amax = fmaxf(amax, fabsf(f[e]));
+    for (int i = 0; i < kHold; ++i) {
+        const int u = lane + i * LANES;
+        if (u < units) {
+            const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
+            held[i].load(src, un.token - at0, r1 - r0, un.dim, a.dh);
+        }
     }
-    amax = block_max(amax, red);
-    const bool begun = off == 0;
+
+    const int slot = slots[r0];
+    if (slot < 0 || (slot >> a.block_shift) >= a.n_blocks || (slot & (size - 1)) != at0) return;
+    const int64_t page = (int64_t)(slot >> a.block_shift) * a.Hkv + hk;
+    // rows that continue the first one
+    int n = r1 - r0;
+    if constexpr (LANES == kWave) {
+        const uint64_t bad = __ballot(lane < n && slots[r0 + min(lane, n - 1)] != slot + lane);
+        if (bad) n = __ffsll((unsigned long long)bad) - 1;
+    } else {
+        if (lane == 0) first_bad = n;
+        __syncthreads();
+        if (lane < n && slots[r0 + lane] != slot + lane) atomicMin(&first_bad, lane);
+        __syncthreads();
+        n = first_bad;
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) {
+        const int u = lane + i * LANES;
+        if (u < units) amax = fmaxf(amax, held[i].largest(unit_at<DP>(q0 * (DP / 8) + u, kind).token - at0, n));
+    }
+    for (int u = lane + kHold * LANES; u < units; u += LANES) {
+        const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
+        Rows<T> rows;
+        rows.load(src, un.token - at0, n, un.dim, a.dh);
+        amax = fmaxf(amax, rows.largest(un.token - at0, n));
+    }
+    amax = wave_max(amax);
+    if constexpr (LANES > kWave) amax = block_max(amax, red);
+
+    const bool begun = at0 == 0;
     float *scale = a.scale[kind] + page;
     int e = scale_exp(amax), e_old = e;
     if (!begun) {
@@ -178,54 +325,97 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(StoreArgs a,
         e_old = min(max(e_old, kScaleExpMin), kScaleExpMax);
         e = max(e, e_old);
     }
-    __syncthreads();
-    if (threadIdx.x == 0) *scale = pow2(e);
+    if constexpr (LANES > kWave) __syncthreads();
+    if (lane == 0) *scale = pow2(e);
     const bool grown = e > e_old;
     const float inv = pow2(-e), shrink = pow2(max(e_old - e, -126));
+    uint8_t *block = a.cache[kind] + page * size * DP;
 
-    // pieces: dp of 16 bytes per group of 16 tokens
-    uint8_t *block = a.cache[kind] + page * size * dp;
-    const int g0 = begun || grown ? 0 : off / kCacheGroup;
-    const int g1 = begun ? size / kCacheGroup : (off + n + kCacheGroup - 1) / kCacheGroup;
-    for (int i = threadIdx.x; i < (g1 - g0) * dp; i += kStoreThreads) {
-        const int group = g0 + i / dp, piece = i % dp;
-        uint4 *dst = reinterpret_cast<uint4 *>(block + (int64_t)(group * dp + piece) * kCacheGroup);
-        uint4 out = begun ? zero16() : *dst;
-        uint32_t *w = &out.x;
-        if (kind == 0) {  // 16 dims of one token
-            const int row = group * kCacheGroup + piece % kCacheGroup - off, d0 = piece / kCacheGroup * 16;
-            if (row >= n || (row < 0 && !grown)) {
-                if (!begun) continue;
-            } else if (row < 0) {
-                for (int j = 0; j < 4; ++j) w[j] = rescale_fp8(w[j], shrink);
-            } else {
-                float f[16];
-                for (int j = 0; j < 16; ++j)
-                    f[j] = d0 + j < a.dh ? load_elem(src + (int64_t)row * a.dh + d0 + j) * inv : 0.f;
-                for (int j = 0; j < 4; ++j) w[j] = to_fp8(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+    // Bytes of a piece's tokens: new ones from `now`, earlier ones as they are or under the larger
+    // scale, later ones zero in a block that is begun and as they are in another.
+    auto write = [&](const Unit &un, const uint4 *now) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = un.piece_token[i] - at0;
+            const uint32_t one = row >= 0 && row < n ? ~0u : 0u;  // k: the token of the piece
+            uint32_t fresh = one, earlier = row < 0 ? ~0u : 0u;
+            if (kind == 1) {
+                fresh = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) fresh |= row + r >= 0 && row + r < n ? 0xffu << (8 * r) : 0u;
+                earlier = row >= 0 ? 0u : row <= -4 ? ~0u : (1u << (8 * -row)) - 1u;
             }
-        } else {  // four tokens of dims d0, d0 + 16, d0 + 32, d0 + 48
-            const int row = group * kCacheGroup + piece / 16 % 4 * 4 - off, d0 = piece / 64 * 64 + piece % 16;
-            if (!begun && (row >= n || (row + 3 < 0 && !grown))) continue;
-            for (int j = 0; j < 4; ++j) {
-                const int d = d0 + 16 * j;
-                float f[4];
-                uint32_t fresh = 0;  // bytes of new tokens
-                for (int r = 0; r < 4; ++r) {
-                    const bool is_new = row + r >= 0 && row + r < n;
-                    fresh |= is_new ? 0xffu << (8 * r) : 0u;
-                    f[r] = is_new && d < a.dh ? load_elem(src + (int64_t)(row + r) * a.dh + d) * inv : 0.f;
+            if (!begun && fresh == 0 && !(grown && earlier)) continue;
+            uint4 *dst = reinterpret_cast<uint4 *>(block + un.piece[i]);
+            uint4 out = zero16();
+            if (!begun && fresh != ~0u) {
+                out = *dst;
+                if (grown && earlier) {
+                    out.x = (rescale_fp8(out.x, shrink) & earlier) | (out.x & ~earlier);
+                    out.y = (rescale_fp8(out.y, shrink) & earlier) | (out.y & ~earlier);
+                    out.z = (rescale_fp8(out.z, shrink) & earlier) | (out.z & ~earlier);
+                    out.w = (rescale_fp8(out.w, shrink) & earlier) | (out.w & ~earlier);
                 }
-                const uint32_t now = to_fp8(f[0], f[1], f[2], f[3]);
-                uint32_t old = w[j];
-                if (grown) {  // bytes of the tokens before the new ones
-                    const uint32_t before = row >= 0 ? 0u : row <= -4 ? ~0u : (1u << (8 * -row)) - 1u;
-                    old = (rescale_fp8(old, shrink) & before) | (old & ~before);
-                }
-                w[j] = (now & fresh) | (old & ~fresh);
             }
+            out.x = (now[i].x & fresh) | (out.x & ~fresh);
+            out.y = (now[i].y & fresh) | (out.y & ~fresh);
+            out.z = (now[i].z & fresh) | (out.z & ~fresh);
+            out.w = (now[i].w & fresh) | (out.w & ~fresh);
+            *dst = out;
         }
-        *dst = out;
+    };
+    // (the exchanges between lanes: units of a quad of lanes end together, a page has a multiple of 8)
+    uint4 now[2];
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) {
+        const int u = lane + i * LANES;
+        if (u < units) {
+            held[i].pieces(kind, inv, now);
+            write(unit_at<DP>(q0 * (DP / 8) + u, kind), now);
+        }
+    }
+    for (int u = lane + kHold * LANES; u < units; u += LANES) {
+        const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
+        Rows<T> rows;
+        rows.load(src, un.token - at0, n, un.dim, a.dh);
+        rows.pieces(kind, inv, now);
+        write(un, now);
+    }
+    now[0] = now[1] = zero16();
+    if (begun)
+        for (int u = q1 * (DP / 8) + lane; u < size / 4 * (DP / 8); u += LANES) write(unit_at<DP>(u, kind), now);
+    else if (grown)
+        for (int u = lane; u < q0 * (DP / 8); u += LANES) write(unit_at<DP>(u, kind), now);
+}
+
+template <typename T, int DP, int LANES, int kHold>
+hipError_t launch_store_as(const StoreArgs &a, hipStream_t s) {
+    const int runs = (a.n_new + (1 << a.block_shift) - 2) / (1 << a.block_shift) + 1;
+    const int pages = 2 * a.B * a.Hkv * runs, per = kStoreThreads / LANES;
+    hipLaunchKernelGGL((cache_store_kernel<T, DP, LANES, kHold>), dim3((pages + per - 1) / per), dim3(kStoreThreads), 0,
+                       s, a, runs, pages);
+    return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t launch_store_dp(const StoreArgs &a, hipStream_t s) {
+    constexpr int kMost = sizeof(T) == 2 ? 4 : 2;  // 64 registers
+    const int size = 1 << a.block_shift;
+    // quads that one call's rows can lie in
+    const int units = min(size / 4, (a.n_new + 6) / 4) * (DP / 8);
+    if (size <= 32)
+        return units <= kWave ? launch_store_as<T, DP, kWave, 1>(a, s) : launch_store_as<T, DP, kWave, kMost>(a, s);
+    return units <= kStoreThreads ? launch_store_as<T, DP, kStoreThreads, 1>(a, s)
+                                  : launch_store_as<T, DP, kStoreThreads, kMost>(a, s);
+}
+
+template <typename T>
+hipError_t launch_store_t(const StoreArgs &a, hipStream_t s) {
+    switch (cache_dp(a.dh)) {
+        case 64: return launch_store_dp<T, 64>(a, s);
+        case 128: return launch_store_dp<T, 128>(a, s);
+        case 192: return launch_store_dp<T, 192>(a, s);
+        default: return launch_store_dp<T, 256>(a, s);
     }
 }
 
@@ -248,13 +438,7 @@ hipError_t launch_cache_tables(const void *args, hipStream_t s) {
 
 hipError_t launch_cache_store(const void *args, hipStream_t s) {
     const StoreArgs &a = *static_cast<const StoreArgs *>(args);
-    const int runs = (a.n_new + (1 << a.block_shift) - 2) / (1 << a.block_shift) + 1;
-    const dim3 grid(a.B * a.Hkv * runs, 2);
-    if (a.is_bf16)
-        hipLaunchKernelGGL(cache_store_kernel<bf16_t>, grid, dim3(kStoreThreads), 0, s, a, cache_dp(a.dh), runs);
-    else
-        hipLaunchKernelGGL(cache_store_kernel<float>, grid, dim3(kStoreThreads), 0, s, a, cache_dp(a.dh), runs);
-    return hipGetLastError();
+    return a.is_bf16 ? launch_store_t<bf16_t>(a, s) : launch_store_t<float>(a, s);
 }
 
 }  // namespace vscan

@@ -365,7 +365,7 @@ int vscan_cache_attend_workspace_size(const vscan_cache_desc *desc, size_t *byte
     if (!bytes) return VSCAN_ERR_NULL;
     AttendPlan p;
     const int rc = plan_attend(desc, &p);
-    if (rc == VSCAN_OK) *bytes = std::max<size_t>(p.bytes, kAlign);
+    if (rc == VSCAN_OK) *bytes = p.bytes;
     return rc;
 }
 

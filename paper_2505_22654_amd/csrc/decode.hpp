@@ -60,24 +60,22 @@ struct AttendArgs {
     float *part_stat;              // [B*Hkv, rows, chunks, 2]: maximum, sum
     int B, Hq, Hkv, T, dh, block_shift, n_blocks, max_blocks, max_len, is_bf16;
     float scale;                   // times log2(e)
-    int row_tiles, split_rows;     // attend_form
-    int row_blocks, chunk, chunks;
+    int row_tiles, row_blocks, chunk, chunks;  // attend_form
 };
-constexpr int kAttendTile = 64;    // keys a wave takes at a time
 constexpr int kAttendWaves = 4;
-// How a call is cut into workgroups: fills the last five fields from the others.
+// Keys that a wave takes at a time, by the tiles of 16 rows that it holds.
+constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
+// How a call is cut into workgroups: fills the last four fields from the others.
 inline void attend_form(AttendArgs &a) {
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
-    const int most = a.is_bf16 ? (a.dh > 128 ? 2 : 4) : (a.dh > 128 ? 1 : 2);
-    a.row_tiles = rows <= 16 ? 1 : rows <= 32 || most < 4 ? (most < 2 ? 1 : 2) : 4;
-    a.split_rows = rows > (int64_t)kCacheGroup * a.row_tiles;
-    const int block = kCacheGroup * a.row_tiles * (a.split_rows ? kAttendWaves : 1);
+    a.row_tiles = rows <= 16 || (!a.is_bf16 && a.dh > 128) ? 1 : 2;
+    const int block = kCacheGroup * a.row_tiles;
     a.row_blocks = (int)((rows + block - 1) / block);
     const int64_t units = (int64_t)a.B * a.Hkv * a.row_blocks;
-    const int step = kAttendTile * (a.split_rows ? 1 : kAttendWaves);
-    int64_t chunks = (1024 + units - 1) / units;
-    const int64_t most_chunks = (a.max_len + step - 1) / step;
-    if (chunks > most_chunks) chunks = most_chunks;
+    const int step = attend_tile(a.row_tiles) * kAttendWaves;
+    const int64_t most = (a.max_len + step - 1) / step;
+    int64_t chunks = units >= 512 ? 1 : (1024 + units - 1) / units;
+    if (chunks > most) chunks = most;
     if (chunks < 1) chunks = 1;
     const int64_t per = ((a.max_len + chunks - 1) / chunks + step - 1) / step * step;
     a.chunk = (int)(per < step ? step : per);

@@ -141,18 +141,21 @@ def store(shape, x, slot_map, values, scales):
             r += n
 
 
-def attend(shape, q, k_rows, v_rows, table, kv_len, new_len):
-    """(out, bound) in 64 bits.  k_rows, v_rows: values with scales, [n_blocks,Hkv,bs,dh].  `bound` is
-    what rounding may move a result by, apart from the last one: with u = 2^-24 a logit of dh products
-    is off by at most (dh + 8) u sum|q k| scale (the products are exact), a weight by that twice and
-    the exponential's 4 u, the two sums by (keys + 64) u, a weight's planes by 2^-18 (two of 8 bits)."""
+def attend(shape, q, k_rows, v_rows, v_scales, table, kv_len, new_len):
+    """(out, bound) in 64 bits.  k_rows, v_rows: values with scales, [n_blocks,Hkv,bs,dh]; v_scales
+    [n_blocks,Hkv].  `bound` is what rounding may move a result by, apart from the last one: with u =
+    2^-24 a logit of dh products is off by at most (dh + 8) u sum|q k| scale (the products are exact),
+    a weight by that twice and the exponential's 4 u, the two sums by (keys + 64) u.  Then the weights'
+    rounding.  fp32: three planes of 8 bits, 2^-26 of a weight.  bf16 calls: fp16, half a step of
+    which is 2^-11 of a weight, or below fp16's normal numbers 2^-25, where the largest weight (with V's
+    scale) that a wave meets is 2^4 or more: 2^-29 of the largest p s, times values of at most 448."""
     bs, T, G = shape.block_size, shape.n_new, shape.q_heads // shape.kv_heads
     dh, u = shape.head_dim, 2.0 ** -24
     scale = shape.scale if shape.scale > 0 else dh ** -0.5
     cap = shape.max_len or shape.max_blocks * bs
     out = torch.zeros(q.shape, dtype=torch.float64, device=q.device)
     bound = torch.zeros_like(out)
-    planes = 2.0 ** -18 if shape.dtype == "bf16" else 2.0 ** -26
+    planes, floor = (2.0 ** -11, 448 * 2.0 ** -29) if shape.dtype == "bf16" else (2.0 ** -26, 0.0)
     for b in range(shape.batch):
         n = T if new_len is None else min(max(int(new_len[b]), 0), T)
         length = min(max(int(kv_len[b]), 0), cap)
@@ -173,5 +176,7 @@ def attend(shape, q, k_rows, v_rows, table, kv_len, new_len):
             off = (x.abs() @ k.abs().T * scale).masked_fill(~seen, 0.0).amax(1, keepdim=True) * (dh + 8) * u
             p = torch.where(seen.any(1, keepdim=True), torch.softmax(logits, 1), 0.0)
             out[b, h, :n] = p @ v
-            bound[b, h, :n] = (p @ v.abs()) * (2 * off + (length + 72) * u + planes)
+            s = torch.where(there, v_scales.double()[block, h // G], 0.0)
+            bound[b, h, :n] = ((p @ v.abs()) * (2 * off + (length + 72) * u + planes)
+                               + length * floor * (p * s).amax(1, keepdim=True))
     return out, bound

@@ -58,7 +58,7 @@ def check(shape, q, cache, table, rows, lens, new, **kw):
     import torch
     kv = i32(lens)
     got = vb.cache_attend(shape, q, cache, table, kv, None if new is None else i32(new), **kw)["out"]
-    want, bound = ref.attend(shape, q, rows["k"], rows["v"], table, lens, new)
+    want, bound = ref.attend(shape, q, rows["k"], rows["v"], cache["v_scale"], table, lens, new)
     torch.cuda.synchronize()
     over = (got.double() - want).abs() - bound - HALF_STEP[shape.dtype] * want.abs()
     assert bool(torch.isfinite(got).all()) and float(over.max()) <= 0, (shape, float(over.max()))
@@ -116,6 +116,38 @@ def test_large_logits_and_scales_far_apart():
     for dtype in ("bf16", "f32"):
         run(dtype, 8, 2, 128, 16, 3, [700, 65], gain=8.0, seed=7)
         run(dtype, 4, 4, 64, 16, 1, [700, 65], spread=30, seed=8)
+
+
+@pytest.mark.parametrize("apart", [12, 30, 90])
+@pytest.mark.parametrize("T", [1, 40])
+def test_all_weight_on_blocks_of_small_values(apart, T):
+    """Values of a few blocks are 2^-apart of the others', and the queries look at those blocks alone."""
+    import torch
+    for dtype in ("bf16", "f32"):
+        lens = [600, 333]
+        shape = wl.CacheShape(dtype, 2, 4, 2, 128, 16, 62, 40, T)
+        q, cache, table, rows = make(shape, lens, 21, spread=0)
+        small = torch.zeros(shape.n_blocks, dtype=torch.bool, device="cuda")
+        small[table[0, [3, 17]].long()] = True
+        small[table[1, [0, 20]].long()] = True
+        cache["v_scale"][small] *= 2.0 ** -apart
+        rows["v"][small] *= 2.0 ** -apart
+        # keys of the small blocks along one direction, the others against it
+        one = torch.zeros(128, dtype=torch.float64, device="cuda")
+        one[::2] = 448.0
+        for sign, at in ((1, small), (-1, ~small)):
+            held = ref.read(cache, shape, "k")[at]
+            new = torch.where(held.isnan(), held, sign * one.expand_as(held))
+            codes = ref.codes(torch.where(new.isnan(), 0.0, new), shape, "k")
+            mark = ref.codes(new.isnan().double(), shape, "k")
+            part = torch.where(mark == 0, codes, 0x7f).view(cache["k"][at].shape)
+            cache["k"][at] = part
+        rows["k"] = (ref.read(cache, shape, "k") * cache["k_scale"].double()[..., None, None])[..., :128]
+        rows["k"] = torch.where(rows["k"].isnan(), 0.0, rows["k"])
+        q = (0.5 + 0.1 * torch.rand_like(q.float())).to(q.dtype)
+        got, want = check(shape, q, cache, table, rows, lens, None)
+        # logits are at least 2 * 64 * 0.5 * 3.5 / sqrt(128) = 19.8 apart: the others weigh 600 e^-19.8 at most
+        assert float(want[:, :, -1].abs().max()) < 100 * 2.0 ** -apart + 5 * 600 * 2.5e-9 and got[:, :, -1].any()
 
 
 def test_max_len_bounds_the_keys():

@@ -43,7 +43,7 @@ class _Layer:
         sh = dataclasses.replace(self.shape, n_new=q.shape[2])
         got = vb.cache_attend(sh, q, self.cache, self.table, self.kv, new_len)["out"]
         rows = self.rows()
-        want, bound = ref.attend(sh, q, rows["k"], rows["v"], self.table, self.kv.tolist(), None if new_len is None else new_len.tolist())
+        want, bound = ref.attend(sh, q, rows["k"], rows["v"], self.cache["v_scale"], self.table, self.kv.tolist(), None if new_len is None else new_len.tolist())
         over = (got.double() - want).abs() - bound - HALF_STEP[sh.dtype] * want.abs()
         assert float(over.max()) <= 0, float(over.max())
         return got

@@ -9,6 +9,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import sys
 from typing import Dict, Optional
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -65,10 +66,11 @@ class RopeDesc(ctypes.Structure):
                 ("batch", ctypes.c_int32), ("seq_len", ctypes.c_int32),
                 ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
-                ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * ROPE_MAX_AXES),
+                ("n_axes", ctypes.c_int32),
+                *[(f"section{i}", ctypes.c_int32) for i in range(ROPE_MAX_AXES)],
                 ("order", ctypes.c_int32), ("pairing", ctypes.c_int32),
-                ("inverse", ctypes.c_int32), ("q_stride", ctypes.c_int64 * 3),
-                ("k_stride", ctypes.c_int64 * 3)]
+                ("inverse", ctypes.c_int32),
+                *[(f"{t}_stride{i}", ctypes.c_int64) for t in "qk" for i in range(3)]]
 
 
 class CacheDesc(ctypes.Structure):
@@ -555,16 +557,16 @@ def _check(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _check_tensor(name: str, t, dtype, shape, device) -> None:
-    """`t` on `device`, contiguous, of this dtype and shape."""
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {device}, got {t.dtype} "
+def _check_tensor(name: str, t, dtype, shape, index: int) -> None:
+    """`t` on CUDA device `index`, contiguous, of this dtype and shape."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous {dtype} {shape} on cuda:{index}, got {t.dtype} "
                          f"{tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
 
 
 def _workspace(workspace, need: int, device):
     """The caller's workspace as it is, or a new one where one is needed."""
-    import torch
+    torch = _torch()
     if workspace is None:
         return torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _check(workspace.device == device and workspace.dtype == torch.uint8 and workspace.is_contiguous(),
@@ -572,35 +574,36 @@ def _workspace(workspace, need: int, device):
     return workspace
 
 
-def _call(entry: str, device, *args) -> None:
-    """Calls `entry` on the current stream of `device`, with that device the current one."""
-    import torch
-    fn, index = getattr(lib(), entry), device.index
+def _call(entry: str, index: int, *args) -> None:
+    """Calls `entry` on the current stream of CUDA device `index`, with that device the current one.
+    (The stream's handle is taken without the object that torch.cuda.current_stream makes around it:
+    4 of the 19 us that a small call took.)"""
+    torch = _torch()
+    fn, stream = getattr(_lib or lib(), entry), torch._C._cuda_getCurrentRawStream
     if index == torch.cuda.current_device():
-        rc = fn(*args, _raw_stream(index))
+        rc = fn(*args, stream(index))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _raw_stream(index))
+        with torch.cuda.device(index):
+            rc = fn(*args, stream(index))
     if rc != VSCAN_OK:
         raise VscanError(rc, entry)
 
 
-def _raw_stream(index: int) -> int:
-    """Handle of the device's current stream, without the stream object that torch.cuda.current_stream
-    makes around it (4 of the 19 us that a small call took)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(index)
+def _torch(modules=sys.modules):
+    """torch, which lib() imports first (an import statement in every small call costs 0.3 us)."""
+    torch = modules.get("torch")
+    if torch is None:
+        import torch
+    return torch
 
 
 def rope_desc(shape, q_stride=(0, 0, 0), k_stride=(0, 0, 0)) -> RopeDesc:
     """Descriptor from a `RopeShape`-like object."""
     n = len(shape.sections)
     _check(1 <= n <= ROPE_MAX_AXES, f"sections: 1 to {ROPE_MAX_AXES} axes, got {n}")
-    sections = (ctypes.c_int32 * ROPE_MAX_AXES)(*shape.sections)
     return RopeDesc(ctypes.sizeof(RopeDesc), _dtype_code(shape.dtype), shape.batch, shape.seq_len,
-                    shape.q_heads, shape.kv_heads, shape.head_dim, shape.rot_dim, n, sections,
-                    shape.order, shape.pairing, shape.inverse, (ctypes.c_int64 * 3)(*q_stride),
-                    (ctypes.c_int64 * 3)(*k_stride))
+                    shape.q_heads, shape.kv_heads, shape.head_dim, shape.rot_dim, n, *shape.sections,
+                    *(0,) * (ROPE_MAX_AXES - n), shape.order, shape.pairing, shape.inverse, *q_stride, *k_stride)
 
 
 def rope_frequencies(rot_dim: int, theta: float = 10000.0, device="cuda"):
@@ -617,19 +620,19 @@ def rope(shape, positions, inv_freq, q=None, k=None, in_place: bool = False,
     inv_freq [rot_dim/2] float64.
 
     Returns q and k turned: new contiguous tensors, those of `out`, or (`in_place`) the inputs."""
-    import torch
+    torch = _torch()
     dt, B, S = _torch_dtype(shape.dtype), shape.batch, shape.seq_len
-    dev, src, dst, strides = positions.device, [None, None], [None, None], [(0, 0, 0), (0, 0, 0)]
+    index, src, dst, strides = positions.get_device(), [None, None], [None, None], [(0, 0, 0), (0, 0, 0)]
     _check(positions.is_cuda, "positions: expected a CUDA tensor")
-    _check_tensor("positions", positions, torch.int32, (len(shape.sections), B, S), dev)
-    _check_tensor("inv_freq", inv_freq, torch.float64, (shape.rot_dim // 2,), dev)
+    _check_tensor("positions", positions, torch.int32, (len(shape.sections), B, S), index)
+    _check_tensor("inv_freq", inv_freq, torch.float64, (shape.rot_dim // 2,), index)
     for i, (name, t, heads) in enumerate((("q", q, shape.q_heads), ("k", k, shape.kv_heads))):
         if heads == 0:
             _check(t is None, f"{name}: the shape has no heads for it")
             continue
         size = (B, heads, S, shape.head_dim)
-        if t is None or t.dtype is not dt or t.shape != size or t.device != dev:
-            raise ValueError(f"{name}: expected {dt} {size} on {dev}")
+        if t is None or t.dtype is not dt or t.shape != size or t.get_device() != index:
+            raise ValueError(f"{name}: expected {dt} {size} on cuda:{index}")
         if not t.is_contiguous():
             *strides[i], entry = t.stride()
             if entry != 1 or not any(strides[i]):  # three zeros would mean a contiguous tensor
@@ -640,12 +643,12 @@ def rope(shape, positions, inv_freq, q=None, k=None, in_place: bool = False,
         else:
             dst[i] = out.get(name) if out else None
             if dst[i] is None:
-                dst[i] = torch.empty(size, dtype=dt, device=dev)
+                dst[i] = t.new_empty(size)
             else:
-                _check_tensor(f"out[{name!r}]", dst[i], dt, size, dev)
+                _check_tensor(f"out[{name!r}]", dst[i], dt, size, index)
     desc = rope_desc(shape, *strides)
     outs = (None, None) if in_place else (_ptr(dst[0]), _ptr(dst[1]))
-    _call("vscan_rope", dev, ctypes.byref(desc), _ptr(src[0]), _ptr(src[1]), positions.data_ptr(),
+    _call("vscan_rope", index, ctypes.byref(desc), _ptr(src[0]), _ptr(src[1]), positions.data_ptr(),
           inv_freq.data_ptr(), *outs)
     return {n: t for n, t in zip("qk", dst) if t is not None}
 
@@ -679,10 +682,10 @@ def cache_alloc(shape, device="cuda") -> Dict[str, object]:
     return cache
 
 
-def _check_cache(shape, cache, device) -> None:
-    import torch
+def _check_cache(shape, cache, index: int) -> None:
+    torch = _torch()
     for n, d, s in _cache_shapes(shape):
-        _check_tensor(n, cache[n], torch.uint8 if d == "uint8" else torch.float32, s, device)
+        _check_tensor(n, cache[n], torch.uint8 if d == "uint8" else torch.float32, s, index)
 
 
 def cache_plan_workspace_size(desc: CacheDesc) -> int:
@@ -700,24 +703,25 @@ def cache_plan(shape, cached_len, new_len, free_blocks, free_head, block_table, 
 
     Returns slot_map [B,n_new], kv_len [B], free_head and missing [1], and block_table.  `out` may hold
     any of the results; its kv_len may be cached_len and its free_head the one passed."""
-    import torch
-    i32, dev, B = torch.int32, block_table.device, shape.batch
+    torch = _torch()
+    i32, dev, index, B = torch.int32, block_table.device, block_table.get_device(), shape.batch
     desc = cache_desc(shape)
     need = cache_plan_workspace_size(desc)
     _check(block_table.is_cuda, "block_table: expected a CUDA tensor")
-    _check_tensor("cached_len", cached_len, i32, (B,), dev)
-    _check_tensor("new_len", new_len, i32, (B,), dev)
-    _check_tensor("free_blocks", free_blocks, i32, (free_blocks.numel(),), dev)
-    _check_tensor("free_head", free_head, i32, (1,), dev)
-    _check_tensor("block_table", block_table, i32, (B, shape.max_blocks), dev)
+    _check_tensor("cached_len", cached_len, i32, (B,), index)
+    _check_tensor("new_len", new_len, i32, (B,), index)
+    _check_tensor("free_blocks", free_blocks, i32, (free_blocks.numel(),), index)
+    _check_tensor("free_head", free_head, i32, (1,), index)
+    _check_tensor("block_table", block_table, i32, (B, shape.max_blocks), index)
     out = dict(out) if out else {}
+    new = dict(zip(("kv_len", "free_head", "missing"), block_table.new_empty(B + 2).split_with_sizes((B, 1, 1))))
     for name, size in (("slot_map", (B, shape.n_new)), ("kv_len", (B,)), ("free_head", (1,)), ("missing", (1,))):
         if name in out:
-            _check_tensor(f"out[{name!r}]", out[name], i32, size, dev)
+            _check_tensor(f"out[{name!r}]", out[name], i32, size, index)
         else:
-            out[name] = torch.empty(size, dtype=i32, device=dev)
+            out[name] = new[name] if name in new else block_table.new_empty(size)
     workspace = _workspace(workspace, need, dev)
-    _call("vscan_cache_plan", dev, ctypes.byref(desc), cached_len.data_ptr(), new_len.data_ptr(),
+    _call("vscan_cache_plan", index, ctypes.byref(desc), cached_len.data_ptr(), new_len.data_ptr(),
           free_blocks.data_ptr(), free_blocks.numel(), free_head.data_ptr(), block_table.data_ptr(),
           out["slot_map"].data_ptr(), out["kv_len"].data_ptr(), out["free_head"].data_ptr(),
           out["missing"].data_ptr(), workspace.data_ptr(), workspace.numel())
@@ -729,12 +733,13 @@ def cache_store(shape, k, v, slot_map, cache) -> Dict[str, object]:
     """vscan_cache_store on CUDA tensors k, v [B,Hkv,n_new,dh], slot_map [B,n_new] int32 and a cache of
     `cache_alloc`, which is written in place and returned.  k and v may be the first n_new rows of longer
     slabs (what an in-place prune returns)."""
-    import torch
-    dt, dev, T, dh = _torch_dtype(shape.dtype), slot_map.device, shape.n_new, shape.head_dim
+    torch = _torch()
+    dt, dev, index = _torch_dtype(shape.dtype), slot_map.device, slot_map.get_device()
+    T, dh = shape.n_new, shape.head_dim
     size, rows = (shape.batch, shape.kv_heads, T, dh), T
     _check(slot_map.is_cuda, "slot_map: expected a CUDA tensor")
     for name, t in (("k", k), ("v", v)):
-        if t.dtype is not dt or t.shape != size or t.device != dev:
+        if t.dtype is not dt or t.shape != size or t.get_device() != index:
             raise ValueError(f"{name}: expected {dt} {size} on {dev}")
     if not (k.is_contiguous() and v.is_contiguous()):
         _check(k.stride() == v.stride() and k.stride(3) == 1 and k.stride(2) == dh and k.stride(1) % dh == 0
@@ -742,10 +747,10 @@ def cache_store(shape, k, v, slot_map, cache) -> Dict[str, object]:
                and (shape.batch == 1 or k.stride(0) == shape.kv_heads * k.stride(1)),
                f"k, v: expected rows of equal slabs, got strides {k.stride()} and {v.stride()}")
         rows = k.stride(1) // dh
-    _check_tensor("slot_map", slot_map, torch.int32, (shape.batch, T), dev)
-    _check_cache(shape, cache, dev)
+    _check_tensor("slot_map", slot_map, torch.int32, (shape.batch, T), index)
+    _check_cache(shape, cache, index)
     desc = cache_desc(shape, rows)
-    _call("vscan_cache_store", dev, ctypes.byref(desc), k.data_ptr(), v.data_ptr(), slot_map.data_ptr(),
+    _call("vscan_cache_store", index, ctypes.byref(desc), k.data_ptr(), v.data_ptr(), slot_map.data_ptr(),
           cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr())
     return cache
 
@@ -764,25 +769,25 @@ def cache_attend(shape, q, cache, block_table, kv_len, new_len=None, workspace=N
     [B,max_blocks], kv_len [B] and new_len [B] int32 (None: n_new everywhere).
 
     Returns out [B,Hq,n_new,dh] and the workspace; both may be passed in."""
-    import torch
-    i32, dt, dev, B = torch.int32, _torch_dtype(shape.dtype), q.device, shape.batch
+    torch = _torch()
+    i32, dt, dev, index, B = torch.int32, _torch_dtype(shape.dtype), q.device, q.get_device(), shape.batch
     desc = cache_desc(shape)
-    need = cache_attend_workspace_size(desc)
     size = (B, shape.q_heads, shape.n_new, shape.head_dim)
     _check(q.is_cuda, "q: expected a CUDA tensor")
-    _check_tensor("q", q, dt, size, dev)
-    _check_tensor("block_table", block_table, i32, (B, shape.max_blocks), dev)
-    _check_tensor("kv_len", kv_len, i32, (B,), dev)
+    _check_tensor("q", q, dt, size, index)
+    _check_tensor("block_table", block_table, i32, (B, shape.max_blocks), index)
+    _check_tensor("kv_len", kv_len, i32, (B,), index)
     if new_len is not None:
-        _check_tensor("new_len", new_len, i32, (B,), dev)
-    _check_cache(shape, cache, dev)
+        _check_tensor("new_len", new_len, i32, (B,), index)
+    _check_cache(shape, cache, index)
+    need = cache_attend_workspace_size(desc) if workspace is None else 0
     workspace = _workspace(workspace, need, dev)
     res = out.get("out") if out else None
     if res is None:
-        res = torch.empty(size, dtype=dt, device=dev)
+        res = q.new_empty(size)
     else:
-        _check_tensor("out", res, dt, size, dev)
-    _call("vscan_cache_attend", dev, ctypes.byref(desc), q.data_ptr(), cache["k"].data_ptr(), cache["v"].data_ptr(),
+        _check_tensor("out", res, dt, size, index)
+    _call("vscan_cache_attend", index, ctypes.byref(desc), q.data_ptr(), cache["k"].data_ptr(), cache["v"].data_ptr(),
           cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
           _ptr(new_len), res.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel())
     return {"out": res, "workspace": workspace}

@@ -143,7 +143,7 @@ struct TileAt {
 };
 
 template <typename T, int DP, int NR, int kTile>
-__global__ __launch_bounds__(kWaves *kWave, DP <= 128 && NR <= 2 && sizeof(T) == 2 ? 2 : 1) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1) void attend_kernel(AttendArgs a) {
     typedef Operand<T> O;
     constexpr int kGroups = kTile / kCacheGroup;
     constexpr int kH = DP / 64;  // 16-byte loads per lane and group
@@ -449,8 +449,8 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && NR <= 2 && sizeof(T) ==
         for (int w = 0; w < kWaves; ++w) f[w] *= inv * pow2(refs[w] - e);
         const float unit = pow2(e);
 #pragma unroll
-        for (int i = 0; i < kD / kWaves; ++i) {
-            const int d = i * kWaves + wave, dim = 16 * d + 4 * g;
+        for (int d = wave; d < kD; d += kWaves) {
+            const int dim = 16 * d + 4 * g;
             f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
@@ -477,16 +477,18 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && NR <= 2 && sizeof(T) ==
     }
 }
 
-// Joins the chunks of a row, each of which is an average with its sum of weights: one thread per four dims.
-constexpr int kCombineThreads = 256;
-template <typename T>
-__global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int dp) {
-    const int per_row = dp / 4;
-    const int64_t id = (int64_t)blockIdx.x * kCombineThreads + threadIdx.x;
-    const int G = a.Hq / a.Hkv, rows = G * a.T;
-    const int64_t row = id / per_row;
-    const int dim = (int)(id % per_row) * 4;
-    if (row >= (int64_t)a.B * a.Hkv * rows || dim >= a.dh) return;
+// Joins the chunks of a row, each of which is an average with its sum of weights.  A wave per row, so
+// many lanes per chunk that they hold its dims four at a time; bound by latency, so the averages are
+// requested before it is known what they weigh.
+constexpr int kCombineThreads = 256, kAhead = 4;
+template <typename T, int DP>
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a) {
+    constexpr int kLanes = DP / 4, kSets = kWave / kLanes;  // lanes of a chunk, chunks at a time
+    const int G = a.Hq / a.Hkv, rows = G * a.T, lane = lane_id();
+    const int64_t row = (int64_t)blockIdx.x * (kCombineThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= (int64_t)a.B * a.Hkv * rows) return;
+    const int set = min(lane / kLanes, kSets - 1), dim = lane % kLanes * 4;
+    const float *stat = a.part_stat + row * a.chunks * 2, *part = a.part_acc + row * a.chunks * DP + dim;
     const int r = (int)(row % rows), t = r / G;
     const int64_t bh = row / rows;
     const int hk = (int)(bh % a.Hkv), b = (int)(bh / a.Hkv);
@@ -494,25 +496,50 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, 
     const int lim = t < sp.n ? max(sp.first + t + 1, 0) : 0;
     const int n = (int)(((int64_t)lim + a.chunk - 1) / a.chunk);
     float mx = kNothing, sum = 0.f;
-    const float *stat = a.part_stat + row * a.chunks * 2;
-    for (int c = 0; c < n; ++c) mx = fmaxf(mx, stat[2 * c]);
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < n; ++c) {
-        const float f = __builtin_amdgcn_exp2f(stat[2 * c] - mx) * stat[2 * c + 1];
-        const float4 x = *reinterpret_cast<const float4 *>(a.part_acc + (row * a.chunks + c) * dp + dim);
-        sum += f;
-        o[0] += f * x.x;
-        o[1] += f * x.y;
-        o[2] += f * x.z;
-        o[3] += f * x.w;
+    for (int c0 = 0; c0 < n; c0 += kAhead * kSets) {
+        float4 x[kAhead];
+        float m[kAhead], l[kAhead], top = kNothing;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int c = c0 + i * kSets + set, at = min(c, n - 1);
+            x[i] = *reinterpret_cast<const float4 *>(part + (int64_t)at * DP);
+            m[i] = c < n ? stat[2 * at] : kNothing;
+            l[i] = c < n ? stat[2 * at + 1] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) top = fmaxf(top, m[i]);
+        const float now = fmaxf(mx, top), keep = __builtin_amdgcn_exp2f(mx - now);
+        mx = now;
+        sum *= keep;
+        o *= keep;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float f = __builtin_amdgcn_exp2f(m[i] - now) * l[i];
+            sum += f;
+            o[0] += f * x[i].x;
+            o[1] += f * x[i].y;
+            o[2] += f * x[i].z;
+            o[3] += f * x[i].w;
+        }
     }
+#pragma unroll
+    for (int d = kLanes; d < kLanes * kSets; d *= 2) {
+        const float other = __shfl_xor(mx, d, kWave), now = fmaxf(mx, other);
+        const float f = __builtin_amdgcn_exp2f(mx - now), fo = __builtin_amdgcn_exp2f(other - now);
+        mx = now;
+        sum = sum * f + __shfl_xor(sum, d, kWave) * fo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * f + __shfl_xor(o[e], d, kWave) * fo;
+    }
+    if (lane >= kLanes || dim >= a.dh) return;
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     const int64_t at = (((int64_t)b * a.Hq + hk * G + (r - t * G)) * a.T + t) * a.dh + dim;
     store4<T>(static_cast<T *>(a.out) + at, o * inv);
 }
 
 template <typename T, int DP, int NR>
-hipError_t launch_nr(const AttendArgs &a, hipStream_t s) {
+hipError_t launch_as(const AttendArgs &a, hipStream_t s) {
     constexpr int kTile = attend_tile(NR);
     const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks * a.chunks));
     constexpr size_t lds = kWaves * (DP / 16) * kWave * 16 + kWaves * 16 * 2 * sizeof(float) + kWaves * sizeof(int);
@@ -528,8 +555,8 @@ hipError_t launch_nr(const AttendArgs &a, hipStream_t s) {
 template <typename T, int DP>
 hipError_t launch_dp(const AttendArgs &a, hipStream_t s) {
     if constexpr (sizeof(T) == 2 || DP <= 128)
-        if (a.row_tiles == 2) return launch_nr<T, DP, 2>(a, s);
-    return a.row_tiles == 1 ? launch_nr<T, DP, 1>(a, s) : hipErrorInvalidValue;
+        if (a.row_tiles == 2) return launch_as<T, DP, 2>(a, s);
+    return launch_as<T, DP, 1>(a, s);
 }
 
 template <typename T>
@@ -540,6 +567,19 @@ hipError_t launch_t(const AttendArgs &a, hipStream_t s) {
         case 192: return launch_dp<T, 192>(a, s);
         default: return launch_dp<T, 256>(a, s);
     }
+}
+
+template <typename T>
+hipError_t launch_combine(const AttendArgs &a, hipStream_t s) {
+    constexpr int kRows = kCombineThreads / kWave;
+    const dim3 grid((unsigned)(((int64_t)a.B * a.Hq * a.T + kRows - 1) / kRows));
+    switch (cache_dp(a.dh)) {
+        case 64: hipLaunchKernelGGL((combine_kernel<T, 64>), grid, dim3(kCombineThreads), 0, s, a); break;
+        case 128: hipLaunchKernelGGL((combine_kernel<T, 128>), grid, dim3(kCombineThreads), 0, s, a); break;
+        case 192: hipLaunchKernelGGL((combine_kernel<T, 192>), grid, dim3(kCombineThreads), 0, s, a); break;
+        default: hipLaunchKernelGGL((combine_kernel<T, 256>), grid, dim3(kCombineThreads), 0, s, a);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -553,14 +593,7 @@ hipError_t launch_cache_attend(const void *args, hipStream_t s) {
 
 hipError_t launch_cache_combine(const void *args, hipStream_t s) {
     const AttendArgs &a = *static_cast<const AttendArgs *>(args);
-    const int dp = cache_dp(a.dh);
-    const int64_t items = (int64_t)a.B * a.Hq * a.T * (dp / 4);
-    const dim3 grid((unsigned)((items + kCombineThreads - 1) / kCombineThreads));
-    if (a.is_bf16)
-        hipLaunchKernelGGL(combine_kernel<bf16_t>, grid, dim3(kCombineThreads), 0, s, a, dp);
-    else
-        hipLaunchKernelGGL(combine_kernel<float>, grid, dim3(kCombineThreads), 0, s, a, dp);
-    return hipGetLastError();
+    return a.is_bf16 ? launch_combine<bf16_t>(a, s) : launch_combine<float>(a, s);
 }
 
 }  // namespace vscan

@@ -146,6 +146,7 @@ template <typename T, int DP, int NR, int kTile>
 __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1) void attend_kernel(AttendArgs a) {
     typedef Operand<T> O;
     constexpr int kGroups = kTile / kCacheGroup;
+    constexpr int kStages = NR > 1 && DP <= 128 ? 2 : 1;  // tiles in flight
     constexpr int kH = DP / 64;  // 16-byte loads per lane and group
     constexpr int kD = DP / 16;  // tiles of 16 dims
     constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes;
@@ -162,14 +163,16 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     const int G = a.Hq / a.Hkv, rows = G * a.T, size = 1 << a.block_shift;
     const int32_t *table = a.block_table + (int64_t)b * a.max_blocks;
 
-    // Block numbers of a tile's groups; read ahead of knowing whether the tokens are there.
-    auto blocks_of = [&](int kt, int *block) {
-#pragma unroll
-        for (int u = 0; u < kGroups; ++u) block[u] = table[min((kt + u * kCacheGroup) >> a.block_shift, a.max_blocks - 1)];
-    };
     const int k0 = chunk * a.chunk, step = kTile * kWaves;
-    int kt = k0 + wave * kTile, block[kGroups];
-    blocks_of(kt, block);
+    int kt = k0 + wave * kTile;
+    // Block numbers of the wave's next kBatch tiles, a group of 16 tokens to a lane; the first are read
+    // ahead of knowing whether the tokens are there.
+    constexpr int kBatch = kWave / kGroups;
+    auto blocks_from = [&](int kt) {
+        const int64_t key = kt + (int64_t)(lane / kGroups) * step + lane % kGroups * kCacheGroup;
+        return table[min(key >> a.block_shift, (int64_t)a.max_blocks - 1)];
+    };
+    int block_ahead = blocks_from(kt);
     const Span sp = span_of(a, b);
 
     // row r is query r / G, head hk * G + r % G
@@ -181,17 +184,36 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     // the joining launch reads the chunks that a row reaches into
     if (a.chunks > 1 && k0 >= reach) return;
 
-    // (what is not there is read from the first page: no load depends on a branch)
-    auto locate = [&](int kt, const int *block, TileAt<kGroups> &at) {
+    // A batch: the lane's block (-1: no such tokens) and its scales, and the next batch's blocks.  Waited
+    // for here, so that no later load of the loop is.
+    int lane_block, located = 0, batch_kt = kt;
+    float lane_ks, lane_vs;
+    auto next_batch = [&]() {
+        const int64_t key = batch_kt + (int64_t)(lane / kGroups) * step + lane % kGroups * kCacheGroup;
+        lane_block = key < k1 && (unsigned)block_ahead < (unsigned)a.n_blocks ? block_ahead : -1;
+        const int64_t page = (int64_t)max(lane_block, 0) * a.Hkv + hk;
+        lane_ks = a.k_scale[page];
+        lane_vs = a.v_scale[page];
+        const int64_t next = batch_kt + (int64_t)kBatch * step;
+        batch_kt = next < k1 ? (int)next : k1;
+        block_ahead = blocks_from(batch_kt);
+        asm volatile("" ::"v"(lane_ks), "v"(lane_vs), "v"(block_ahead));
+    };
+    // Where a tile lies (what is not there is read from the first page: no load depends on a branch).
+    auto locate = [&](int kt, TileAt<kGroups> &at) {
+        if (located == kBatch) {
+            next_batch();
+            located = 0;
+        }
 #pragma unroll
         for (int u = 0; u < kGroups; ++u) {
-            const int key = kt + u * kCacheGroup;
-            at.there[u] = key < k1 && (unsigned)block[u] < (unsigned)a.n_blocks;
-            const int64_t page = at.there[u] ? (int64_t)block[u] * a.Hkv + hk : 0;
-            at.base[u] = (page * size + (key & (size - 1))) * DP;
-            at.ks[u] = a.k_scale[page];
-            at.vs[u] = a.v_scale[page];
+            const int from = located * kGroups + u, block = __builtin_amdgcn_readlane(lane_block, from);
+            at.there[u] = block >= 0;
+            at.base[u] = (((int64_t)max(block, 0) * a.Hkv + hk) * size + ((kt + u * kCacheGroup) & (size - 1))) * DP;
+            at.ks[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_ks), from));
+            at.vs[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_vs), from));
         }
+        ++located;
     };
     auto fetch = [&](const uint8_t *cache, const TileAt<kGroups> &at, uint4 (*to)[kH]) {
 #pragma unroll
@@ -199,15 +221,6 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 #pragma unroll
             for (int h = 0; h < kH; ++h) to[u][h] = load16(cache + at.base[u], h * 1024 + lane * 16);
     };
-    TileAt<kGroups> at;
-    uint4 kb[kGroups][kH], vb[kGroups][kH];
-    if (kt < k1) {
-        locate(kt, block, at);
-        fetch(a.k_cache, at, kb);
-        fetch(a.v_cache, at, vb);
-        blocks_of(kt + step, block);
-    }
-
     bf16x8_t qf[NR][2 * kH][kQ];
     int lim[NR];
     int64_t row_at[NR];  // element offset of the row in q and out; < 0: no such row
@@ -250,6 +263,25 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
     }
 
+    TileAt<kGroups> ats[kStages];
+    uint4 kbs[kStages][kGroups][kH], vbs[kStages][kGroups][kH];
+    if (kt < k1) {
+        next_batch();
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) {
+            locate(kt + i * step, ats[i]);
+            fetch(a.k_cache, ats[i], kbs[i]);
+            fetch(a.v_cache, ats[i], vbs[i]);
+        }
+    }
+    // (the queries are waited for here, not in the loop)
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+        for (int c = 0; c < 2 * kH; ++c)
+#pragma unroll
+            for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[nr][c][q]));
+
     f32x4_t acc[NR][kD];
     float m[NR], l[NR];
     int eref = kScaleExpMin;  // acc holds sums in units of 2^eref
@@ -262,7 +294,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     }
 
     // A tile; kMask: some of its tokens are not there or not seen by every row.
-    auto tile = [&](auto masked, int kt, const TileAt<kGroups> &next) {
+    auto tile = [&](auto masked, const TileAt<kGroups> &at, uint4 (*kb)[kH], uint4 (*vb)[kH], const TileAt<kGroups> &next) {
         constexpr bool kMask = decltype(masked)::value;
         f32x4_t s[NR][kGroups];
 #pragma unroll
@@ -391,23 +423,30 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         fetch(a.v_cache, next, vb);
     };
 
-    // tiles that every row sees whole, as far as all their blocks are there; then the others
-    auto advance = [&](auto masked) {
+    // The tile of a stage, after which the stage takes the tile kStages steps on.
+    auto advance = [&](auto masked, int stage) {
         TileAt<kGroups> next;
-        locate(kt + step, block, next);
-        blocks_of(kt + 2 * step, block);
-        tile(masked, kt, next);
-        at = next;
+        locate(kt + kStages * step, next);
+        tile(masked, ats[stage], kbs[stage], vbs[stage], next);
+        ats[stage] = next;
         kt += step;
     };
-    for (; kt + kTile <= min(k1, all_see); ) {
+    // tiles that every row sees whole, as far as all their blocks are there; then the others
+    while (kt + (kStages - 1) * step + kTile <= min(k1, all_see)) {
         bool whole = true;
 #pragma unroll
-        for (int u = 0; u < kGroups; ++u) whole = whole && at.there[u];
+        for (int i = 0; i < kStages; ++i)
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u) whole = whole && ats[i].there[u];
         if (!whole) break;
-        advance(std::false_type());
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) advance(std::false_type(), i);
     }
-    while (kt < k1) advance(std::true_type());
+    while (kt < k1) {
+#pragma unroll
+        for (int i = 0; i < kStages; ++i)
+            if (kt < k1) advance(std::true_type(), i);
+    }
 
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr) {

@@ -422,8 +422,9 @@ typedef struct {
     int32_t seq_len;        /* vscan_cache_store: rows between the slabs of k and v,
                                >= n_new (0: n_new) */
     int32_t max_len;        /* vscan_cache_attend: no sequence holds more tokens than
-                               this (longer ones are cut to it); 0: max_blocks *
-                               block_size.  A close bound makes calls faster. */
+                               this (longer ones are cut to it), at most 2^30; 0:
+                               max_blocks * block_size.  A close bound makes calls
+                               faster. */
     float scale;            /* logit scale; <= 0 selects 1/sqrt(head_dim) */
 } vscan_cache_desc;
 

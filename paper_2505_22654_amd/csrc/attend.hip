@@ -1,10 +1,9 @@
 // Attention of a few or many queries over the paged 8-bit cache.
 //
-// Rows are the (query, query head) pairs of one kv head, 16 to a matrix tile.  S^T = K Q^T with
-// 16x16x32 instructions, whose accumulators hold, for lane (j, g), the logits of row j and tokens
-// 4g .. 4g+3 of each group of 16 - which is the operand layout of O^T = V^T P^T, so the weights never
-// leave the lane's registers.  The cache is stored in operand order: a lane's 16 bytes are one load, a
-// wave's load is 1 KiB in a row, and nothing is staged in LDS.
+// Rows are the (query, query head) pairs of one kv head.  S^T = K Q^T and O^T = V^T P^T: the
+// accumulators of the first product hold a row's weights in the lanes and order in which the second
+// takes them, so they never leave the registers.  The cache is stored in operand order: a lane's 16
+// bytes are one load, and nothing is staged in LDS.
 //
 // bf16 calls: K as bf16 (exact) times q; V as fp16 (exact) times the weights in fp16 (2^-11 of each;
 // bf16's 2^-8 would add as much to the error as the result's own rounding).  fp32 calls: q and the
@@ -14,11 +13,15 @@
 // Softmax in one pass against a reference that is raised only where a logit passes it by more than
 // 2^8, so that most tiles need no exchange between lanes.
 //
+// Two forms, by rows: up to 16, with 16x16x32 instructions and 64 keys at a time (bound by HBM: 2 dh
+// bytes per token and kv head); more, 32 to a workgroup, with 32x32x16 instructions and 32 keys at a
+// time, two tiles in flight (bound by the vector instructions beside the matrix pipe: per logit a
+// multiply-add, a maximum, an exponential and a sum, and the conversions; a matrix instruction keeps the
+// vector unit from issuing for some cycles whatever its size, so the large ones overlap better: 96
+// multiply-adds and 16 exponentials with 514 cycles of them 667, with 16x16x32 861).
 // The four waves of a workgroup take the tiles of its keys in turn and add their results in LDS; where
 // sequences and rows leave compute units idle the keys are cut into chunks over workgroups, which a
-// second launch joins.  Few rows: bound by HBM (2 dh bytes per token and kv head).  Many rows: by the
-// vector instructions beside the matrix pipe (per logit a multiply-add, a maximum, an exponential and
-// a sum, and the conversions).
+// second launch joins.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -57,6 +60,9 @@ struct Operand<bf16_t> {
     static __device__ __forceinline__ f32x4_t mfma(vec a, vec b, f32x4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
+    static __device__ __forceinline__ f32x16_t mfma32(vec a, vec b, f32x16_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
 };
 template <>
 struct Operand<float> {
@@ -68,6 +74,9 @@ struct Operand<float> {
     }
     static __device__ __forceinline__ f32x4_t mfma(vec a, vec b, f32x4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16_t mfma32(vec a, vec b, f32x16_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
 };
 
@@ -95,6 +104,16 @@ __device__ __forceinline__ void split(f32x2_t x, typename O::pair *out) {
             x[1] -= (float)out[p][1];
         }
     }
+}
+
+// Waits until the last register of a product is there for the vector unit.  (The wait states that the
+// compiler leaves by itself, 12 after a 32x32x16, were one tile in some too few where it went on to read
+// an accumulator from its last register: dims 123 and 127 of a row were wrong by a late product.)
+template <int kStates>
+__device__ __forceinline__ void settle_products() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop %0" ::"n"(kStates - 1));
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // Exponent of a power of two.
@@ -134,245 +153,384 @@ __device__ __forceinline__ void store4<bf16_t>(bf16_t *p, f32x4_t v) {
     *reinterpret_cast<uint2 *>(p) = o.u;
 }
 
+// What a workgroup works on: rows of a kv head, and a chunk of its sequence's keys.
+struct Work {
+    int chunk, hk, b, G, rows, row0;
+    int k0, k1;          // keys of the chunk that the last row sees
+    int all_see, reach;  // keys that every row sees, and the last one
+    int block_reach;     // .. and the last row of the workgroup
+    Span sp;
+};
+template <int kRows, int kRowWaves>
+__device__ __forceinline__ Work work_of(const AttendArgs &a, int row_wave) {
+    Work w;
+    int id = blockIdx.x;
+    w.chunk = id % a.chunks;
+    id /= a.chunks;
+    const int block0 = id % a.row_blocks * (kRows * kRowWaves);
+    id /= a.row_blocks;
+    w.hk = id % a.Hkv;
+    w.b = id / a.Hkv;
+    w.G = a.Hq / a.Hkv;
+    w.rows = w.G * a.T;
+    w.sp = span_of(a, w.b);
+    // row r is query r / G, head hk * G + r % G
+    w.row0 = block0 + row_wave * kRows;
+    auto sees = [&](int r) {
+        const int t = min((min(r, w.rows) - 1) / w.G, w.sp.n - 1);  // the last query before row r
+        return max(w.sp.first + t + 1, 0);
+    };
+    const int t0 = w.row0 / w.G;
+    const bool any = w.row0 < w.rows && t0 < w.sp.n;
+    w.reach = any ? sees(w.row0 + kRows) : 0;
+    w.all_see = any ? max(w.sp.first + t0 + 1, 0) : 0;
+    w.block_reach = kRowWaves == 1 ? w.reach : block0 / w.G < w.sp.n ? sees(block0 + kRows * kRowWaves) : 0;
+    w.k0 = w.chunk * a.chunk;
+    w.k1 = min(w.k0 + a.chunk, w.reach);
+    return w;
+}
+
+// A row of a lane.
+struct Row {
+    int64_t at;    // element offset in q and out; < 0: no such row
+    int lim;       // keys it sees
+    bool padding;  // past new_len: written as zero
+};
+__device__ __forceinline__ Row row_of(const AttendArgs &a, const Work &w, int r) {
+    Row x;
+    const int t = r / w.G, head = w.hk * w.G + (r - t * w.G);
+    const bool here = r < w.rows;
+    x.at = here ? (((int64_t)w.b * a.Hq + head) * a.T + t) * a.dh : -1;
+    x.padding = t >= w.sp.n;
+    x.lim = here && !x.padding ? max(w.sp.first + t + 1, 0) : w.reach;
+    return x;
+}
+
+// Eight entries of a query as planes.
+template <typename T>
+__device__ __forceinline__ void load_query(const AttendArgs &a, const Row &row, int d, bf16x8_t *out) {
+    const bool ok = row.at >= 0 && d < a.dh;
+    const T *src = static_cast<const T *>(a.q) + max(row.at, (int64_t)0);
+    if constexpr (sizeof(T) == 2) {
+        union {
+            uint4 u;
+            bf16x8_t v;
+        } raw;
+        raw.u = load16_guard(src, (int64_t)d * 2, ok);
+        out[0] = raw.v;
+    } else {
+        float f[8];
+        unpack16<float>(load16_guard(src, (int64_t)d * 4, ok), f);
+        unpack16<float>(load16_guard(src, (int64_t)d * 4 + 16, ok), f + 4);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            bf16x2_t p[3];
+            split<Operand<float>, 3>(f32x2_t{f[e], f[e + 1]}, p);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                out[q][e] = p[q][0];
+                out[q][e + 1] = p[q][1];
+            }
+        }
+    }
+}
+
 // The keys of a tile: where its groups of 16 lie, and their scales.
 template <int kGroups>
 struct TileAt {
     int64_t base[kGroups];  // bytes from the start of k_cache / v_cache
-    float ks[kGroups], vs[kGroups];
+    float c[kGroups];       // factor of its logits
+    int e[kGroups];         // exponent of V's scale
     bool there[kGroups];
 };
 
-template <typename T, int DP, int NR, int kTile>
-__global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1) void attend_kernel(AttendArgs a) {
-    typedef Operand<T> O;
+// The tiles of a wave: `step` keys apart.  Block numbers and scales of its next 64 groups of 16 tokens
+// are kept a group to a lane, so that a tile's come without a load.
+template <int kGroups, int DP>
+struct Walk {
+    static constexpr int kBatch = kWave / kGroups;  // tiles
+    const AttendArgs &a;
+    const int32_t *table;
+    int hk, step, k1, batch_kt, located = 0, block_ahead, lane_block, lane_e;
+    float lane_c;
+
+    __device__ __forceinline__ Walk(const AttendArgs &args, int b, int hk_, int step_, int kt)
+        : a(args), table(args.block_table + (int64_t)b * args.max_blocks), hk(hk_), step(step_), batch_kt(kt) {
+        block_ahead = blocks_from();  // ahead of knowing whether the tokens are there
+    }
+    __device__ __forceinline__ int64_t lane_key() const {
+        return batch_kt + (int64_t)(lane_id() / kGroups) * step + lane_id() % kGroups * kCacheGroup;
+    }
+    __device__ __forceinline__ int blocks_from() const {
+        return table[min(lane_key() >> a.block_shift, (int64_t)a.max_blocks - 1)];
+    }
+    // A batch: the lane's block (-1: no such tokens) and its scales, and the next batch's blocks.
+    __device__ __forceinline__ void next_batch() {
+        lane_block = lane_key() < k1 && (unsigned)block_ahead < (unsigned)a.n_blocks ? block_ahead : -1;
+        const int64_t page = (int64_t)max(lane_block, 0) * a.Hkv + hk;
+        lane_c = a.k_scale[page];
+        lane_e = __float_as_int(a.v_scale[page]);
+        const int64_t next = batch_kt + (int64_t)kBatch * step;
+        batch_kt = next < k1 ? (int)next : k1;
+        block_ahead = blocks_from();
+        located = 0;
+    }
+    // (waited for at once, so that no later load of the loop is)
+    __device__ __forceinline__ void settle() {
+        lane_c *= a.scale;
+        lane_e = lane_block >= 0 ? exp_of(__int_as_float(lane_e)) : kScaleExpMin;
+        asm volatile("" ::"v"(block_ahead));
+    }
+    // Where the next tile lies, at key kt (what is not there is read from the first page: no load depends
+    // on a branch).
+    __device__ __forceinline__ void locate(int kt, TileAt<kGroups> &at) {
+        if (located == kBatch) {
+            next_batch();
+            settle();
+        }
+        const int size = 1 << a.block_shift;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            const int block = __builtin_amdgcn_readlane(lane_block, located * kGroups + u);
+            at.there[u] = block >= 0;
+            at.base[u] = (((int64_t)max(block, 0) * a.Hkv + hk) * size + ((kt + u * kCacheGroup) & (size - 1))) * DP;
+        }
+        scales_of(located, at);
+        ++located;
+    }
+    __device__ __forceinline__ void scales_of(int tile, TileAt<kGroups> &at) const {
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            at.c[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_c), tile * kGroups + u));
+            at.e[u] = __builtin_amdgcn_readlane(lane_e, tile * kGroups + u);
+        }
+    }
+    // The first kStages tiles: their keys and values are requested before their scales have come.
+    template <int kStages, typename Fetch>
+    __device__ __forceinline__ void begin(int kt, int end, TileAt<kGroups> *ats, Fetch fetch) {
+        k1 = end;
+        next_batch();
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) {
+            locate(kt + i * step, ats[i]);
+            fetch(i);
+        }
+        settle();
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) scales_of(i, ats[i]);
+    }
+};
+
+// V's scales relative to 2^eref: as a factor of the values, and of the weights as an exponent in their
+// logits, which the sums are freed of again.
+template <int kGroups, bool kSplitScale>
+struct Scales {
+    float values[kGroups], weights[kGroups], sums[kGroups];
+    int now;  // eref with this tile's scales
+    __device__ __forceinline__ void of(const TileAt<kGroups> &at, int eref) {
+        now = eref;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) now = max(now, at.e[u]);
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            const int e = at.e[u] - now, w = kSplitScale ? max(min(e - kValueExp, 0), kWeightExp) : 0;
+            values[u] = pow2(e - w);
+            weights[u] = (float)w;
+            sums[u] = pow2(-w);
+        }
+    }
+};
+
+// Walks over the wave's tiles: whole ones, which every row sees and whose blocks are all there, without
+// masks, as far as they come first; then the others.
+template <int kTile, int kStages, typename At, typename Tile>
+__device__ __forceinline__ void walk_tiles(int kt, int step, const Work &w, const At *ats, Tile tile) {
     constexpr int kGroups = kTile / kCacheGroup;
-    constexpr int kStages = NR > 1 && DP <= 128 ? 2 : 1;  // tiles in flight
+    while (kt + (kStages - 1) * step + kTile <= min(w.k1, w.all_see)) {
+        bool whole = true;
+#pragma unroll
+        for (int i = 0; i < kStages; ++i)
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u) whole = whole && ats[i].there[u];
+        if (!whole) break;
+#pragma unroll
+        for (int i = 0; i < kStages; ++i, kt += step) tile(std::false_type(), i, kt);
+    }
+    while (kt < w.k1) {
+#pragma unroll
+        for (int i = 0; i < kStages; ++i)
+            if (kt < w.k1) {
+                tile(std::true_type(), i, kt);
+                kt += step;
+            }
+    }
+}
+
+// Bytes of four tokens of V that are there: those from `left` on lie behind the last one, or not there.
+__device__ __forceinline__ uint32_t value_mask(int left, bool there) {
+    return left <= 0 || !there ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1u;
+}
+
+// The results of the waves of a workgroup for a lane's row, from (reference, sum) pairs and scale
+// references in LDS: factors of their accumulators, and what the row has in all.
+template <int kN>
+struct Joined {
+    float f[kN], mx, sum, unit;
+};
+template <int kN>
+__device__ __forceinline__ Joined<kN> join_waves(const float *stat, const int *refs, int rows, int j, bool padding) {
+    Joined<kN> r;
+    int e = kScaleExpMin;
+    r.mx = kNothing;
+    r.sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kN; ++w) {
+        r.mx = fmaxf(r.mx, stat[(w * rows + j) * 2]);
+        e = max(e, refs[w]);
+    }
+#pragma unroll
+    for (int w = 0; w < kN; ++w) {
+        r.f[w] = __builtin_amdgcn_exp2f(stat[(w * rows + j) * 2] - r.mx);
+        r.sum += r.f[w] * stat[(w * rows + j) * 2 + 1];
+    }
+    // a row without keys, or past new_len, is zero
+    const float inv = r.sum > 0.f && !padding ? 1.f / r.sum : 0.f;
+#pragma unroll
+    for (int w = 0; w < kN; ++w) r.f[w] *= inv * pow2(refs[w] - e);
+    r.unit = pow2(e);
+    return r;
+}
+// Four dims of a row: `at` are the waves' accumulators, `stride` apart.
+template <typename T, int DP, int kN>
+__device__ __forceinline__ void write_row(const AttendArgs &a, const Work &w, const Row &row, int r, int dim,
+                                          const Joined<kN> &jn, const float4 *at, int stride, bool first) {
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < kN; ++v) {
+        const float4 y = at[v * stride];
+        o[0] += jn.f[v] * y.x;
+        o[1] += jn.f[v] * y.y;
+        o[2] += jn.f[v] * y.z;
+        o[3] += jn.f[v] * y.w;
+    }
+    o *= jn.unit;
+    if (row.at < 0) return;
+    if (a.chunks == 1) {
+        if (dim < a.dh) store4<T>(static_cast<T *>(a.out) + row.at + dim, o);
+        return;
+    }
+    // the chunk's result, with its reference and sum, for the joining launch
+    const int64_t part = (((int64_t)w.b * a.Hkv + w.hk) * w.rows + r) * a.chunks + w.chunk;
+    store4<float>(a.part_acc + part * DP + dim, o);
+    if (first) {
+        a.part_stat[2 * part] = jn.mx;
+        a.part_stat[2 * part + 1] = jn.sum;
+    }
+}
+
+// Up to 16 rows.  Lane (j, g) = (lane % 16, lane / 16): row j; of each group of 16 tokens logits of tokens
+// 4g .. 4g+3; of O^T dims 16d + 4g .. +3 of its tiles d.
+template <typename T, int DP>
+__global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1) void attend_few_kernel(AttendArgs a) {
+    typedef Operand<T> O;
+    constexpr int kTile = attend_tile(1), kGroups = kTile / kCacheGroup;
     constexpr int kH = DP / 64;  // 16-byte loads per lane and group
     constexpr int kD = DP / 16;  // tiles of 16 dims
-    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes;
+    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes, step = kTile * kWaves;
     extern __shared__ float4 lds4[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lane_id(), j = lane & 15, g = lane >> 4;
-    int id = blockIdx.x;
-    const int chunk = id % a.chunks;
-    id /= a.chunks;
-    const int rb = id % a.row_blocks;
-    id /= a.row_blocks;
-    const int hk = id % a.Hkv, b = id / a.Hkv;
-    const int G = a.Hq / a.Hkv, rows = G * a.T, size = 1 << a.block_shift;
-    const int32_t *table = a.block_table + (int64_t)b * a.max_blocks;
-
-    const int k0 = chunk * a.chunk, step = kTile * kWaves;
-    int kt = k0 + wave * kTile;
-    // Block numbers of the wave's next kBatch tiles, a group of 16 tokens to a lane; the first are read
-    // ahead of knowing whether the tokens are there.
-    constexpr int kBatch = kWave / kGroups;
-    auto blocks_from = [&](int kt) {
-        const int64_t key = kt + (int64_t)(lane / kGroups) * step + lane % kGroups * kCacheGroup;
-        return table[min(key >> a.block_shift, (int64_t)a.max_blocks - 1)];
-    };
-    int block_ahead = blocks_from(kt);
-    const Span sp = span_of(a, b);
-
-    // row r is query r / G, head hk * G + r % G
-    const int row0 = rb * 16 * NR;
-    const int t0 = row0 / G, t1 = min((min(row0 + 16 * NR, rows) - 1) / G, sp.n - 1);
-    const int reach = t0 <= t1 ? max(sp.first + t1 + 1, 0) : 0;    // keys the last row sees
-    const int all_see = t0 <= t1 ? max(sp.first + t0 + 1, 0) : 0;  // keys every row sees
-    const int k1 = min(k0 + a.chunk, reach);
+    const int chunk = blockIdx.x % a.chunks, hk = blockIdx.x / a.chunks / a.row_blocks % a.Hkv;
+    const int kt0 = chunk * a.chunk + wave * kTile;
+    Walk<kGroups, DP> walk(a, blockIdx.x / a.chunks / a.row_blocks / a.Hkv, hk, step, kt0);
+    const Work w = work_of<16, 1>(a, 0);
     // the joining launch reads the chunks that a row reaches into
-    if (a.chunks > 1 && k0 >= reach) return;
+    if (a.chunks > 1 && w.k0 >= w.reach) return;
 
-    // A batch: the lane's block (-1: no such tokens) and its scales, and the next batch's blocks.  Waited
-    // for here, so that no later load of the loop is.
-    int lane_block, located = 0, batch_kt = kt;
-    float lane_ks, lane_vs;
-    auto next_batch = [&]() {
-        const int64_t key = batch_kt + (int64_t)(lane / kGroups) * step + lane % kGroups * kCacheGroup;
-        lane_block = key < k1 && (unsigned)block_ahead < (unsigned)a.n_blocks ? block_ahead : -1;
-        const int64_t page = (int64_t)max(lane_block, 0) * a.Hkv + hk;
-        lane_ks = a.k_scale[page];
-        lane_vs = a.v_scale[page];
-        const int64_t next = batch_kt + (int64_t)kBatch * step;
-        batch_kt = next < k1 ? (int)next : k1;
-        block_ahead = blocks_from(batch_kt);
-        asm volatile("" ::"v"(lane_ks), "v"(lane_vs), "v"(block_ahead));
-    };
-    // Where a tile lies (what is not there is read from the first page: no load depends on a branch).
-    auto locate = [&](int kt, TileAt<kGroups> &at) {
-        if (located == kBatch) {
-            next_batch();
-            located = 0;
-        }
+    const Row row = row_of(a, w, w.row0 + j);
+    bf16x8_t qf[2 * kH][kQ];
 #pragma unroll
-        for (int u = 0; u < kGroups; ++u) {
-            const int from = located * kGroups + u, block = __builtin_amdgcn_readlane(lane_block, from);
-            at.there[u] = block >= 0;
-            at.base[u] = (((int64_t)max(block, 0) * a.Hkv + hk) * size + ((kt + u * kCacheGroup) & (size - 1))) * DP;
-            at.ks[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_ks), from));
-            at.vs[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_vs), from));
-        }
-        ++located;
-    };
+    for (int c = 0; c < 2 * kH; ++c) load_query<T>(a, row, (c >> 1) * 64 + g * 16 + (c & 1) * 8, qf[c]);
+
     auto fetch = [&](const uint8_t *cache, const TileAt<kGroups> &at, uint4 (*to)[kH]) {
 #pragma unroll
         for (int u = 0; u < kGroups; ++u)
 #pragma unroll
             for (int h = 0; h < kH; ++h) to[u][h] = load16(cache + at.base[u], h * 1024 + lane * 16);
     };
-    bf16x8_t qf[NR][2 * kH][kQ];
-    int lim[NR];
-    int64_t row_at[NR];  // element offset of the row in q and out; < 0: no such row
-    bool padding[NR];    // a row past new_len: written as zero
-#pragma unroll
-    for (int nr = 0; nr < NR; ++nr) {
-        const int r = row0 + nr * 16 + j;
-        const int t = r / G, head = hk * G + (r - t * G);
-        const bool here = r < rows;
-        row_at[nr] = here ? (((int64_t)b * a.Hq + head) * a.T + t) * a.dh : -1;
-        padding[nr] = t >= sp.n;
-        lim[nr] = here && !padding[nr] ? max(sp.first + t + 1, 0) : reach;
-        const T *src = static_cast<const T *>(a.q) + (here ? row_at[nr] : 0);
-#pragma unroll
-        for (int c = 0; c < 2 * kH; ++c) {
-            const int d = (c >> 1) * 64 + g * 16 + (c & 1) * 8;
-            const bool ok = here && d < a.dh;
-            if constexpr (kQ == 1) {
-                union {
-                    uint4 u;
-                    bf16x8_t v;
-                } raw;
-                raw.u = load16_guard(src, (int64_t)d * 2, ok);
-                qf[nr][c][0] = raw.v;
-            } else {
-                float f[8];
-                unpack16<float>(load16_guard(src, (int64_t)d * 4, ok), f);
-                unpack16<float>(load16_guard(src, (int64_t)d * 4 + 16, ok), f + 4);
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    bf16x2_t p[kQ];
-                    split<Operand<float>, kQ>(f32x2_t{f[e], f[e + 1]}, p);
-#pragma unroll
-                    for (int q = 0; q < kQ; ++q) {
-                        qf[nr][c][q][e] = p[q][0];
-                        qf[nr][c][q][e + 1] = p[q][1];
-                    }
-                }
-            }
-        }
-    }
-
-    TileAt<kGroups> ats[kStages];
-    uint4 kbs[kStages][kGroups][kH], vbs[kStages][kGroups][kH];
-    if (kt < k1) {
-        next_batch();
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) {
-            locate(kt + i * step, ats[i]);
-            fetch(a.k_cache, ats[i], kbs[i]);
-            fetch(a.v_cache, ats[i], vbs[i]);
-        }
+    TileAt<kGroups> at[1];
+    uint4 kb[kGroups][kH], vb[kGroups][kH];
+    if (kt0 < w.k1) {
+        walk.template begin<1>(kt0, w.k1, at, [&](int) {
+            fetch(a.k_cache, at[0], kb);
+            fetch(a.v_cache, at[0], vb);
+        });
     }
     // (the queries are waited for here, not in the loop)
 #pragma unroll
-    for (int nr = 0; nr < NR; ++nr)
+    for (int c = 0; c < 2 * kH; ++c)
 #pragma unroll
-        for (int c = 0; c < 2 * kH; ++c)
-#pragma unroll
-            for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[nr][c][q]));
+        for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[c][q]));
 
-    f32x4_t acc[NR][kD];
-    float m[NR], l[NR];
+    f32x4_t acc[kD];
+    float m = kNothing, l = 0.f;
     int eref = kScaleExpMin;  // acc holds sums in units of 2^eref
 #pragma unroll
-    for (int nr = 0; nr < NR; ++nr) {
-        m[nr] = kNothing;
-        l[nr] = 0.f;
-#pragma unroll
-        for (int d = 0; d < kD; ++d) acc[nr][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int d = 0; d < kD; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    // A tile; kMask: some of its tokens are not there or not seen by every row.
-    auto tile = [&](auto masked, const TileAt<kGroups> &at, uint4 (*kb)[kH], uint4 (*vb)[kH], const TileAt<kGroups> &next) {
+    walk_tiles<kTile, 1>(kt0, step, w, at, [&](auto masked, int, int kt) {
         constexpr bool kMask = decltype(masked)::value;
-        f32x4_t s[NR][kGroups];
+        TileAt<kGroups> next;
+        walk.locate(kt + step, next);
+        f32x4_t s[kGroups];
 #pragma unroll
         for (int u = 0; u < kGroups; ++u) {
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) s[nr][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            s[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < 2 * kH; ++c) {
                 const bf16x8_t ka = from_fp8<Operand<float>>(word(kb[u][c >> 1], 2 * (c & 1)), word(kb[u][c >> 1], 2 * (c & 1) + 1), 1.f, 1.f);
 #pragma unroll
-                for (int q = kQ - 1; q >= 0; --q)
-#pragma unroll
-                    for (int nr = 0; nr < NR; ++nr)
-                        s[nr][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[nr][c][q], s[nr][u], 0, 0, 0);
+                for (int q = kQ - 1; q >= 0; --q) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[c][q], s[u], 0, 0, 0);
             }
         }
         fetch(a.k_cache, next, kb);
 
-        // V's scale relative to 2^eref: as a factor of the values, and of the weights as an exponent in
-        // their logits, which the sums are freed of again
-        float c[kGroups], va[kGroups], we[kGroups], wi[kGroups];
-        int top_e = kScaleExpMin;
-#pragma unroll
-        for (int u = 0; u < kGroups; ++u) {
-            c[u] = at.ks[u] * a.scale;
-            if (!kMask || at.there[u]) top_e = max(top_e, exp_of(at.vs[u]));
-        }
-        const int now_e = max(eref, top_e);
-#pragma unroll
-        for (int u = 0; u < kGroups; ++u) {
-            const int e = exp_of(at.vs[u]) - now_e, w = kP == 1 ? max(min(e - kValueExp, 0), kWeightExp) : 0;
-            va[u] = pow2(e - w);
-            we[u] = (float)w;
-            wi[u] = pow2(-w);
-        }
-
-        float x[NR][kGroups * 4];
-        auto logits = [&](int nr, float ref) {
+        Scales<kGroups, kP == 1> sc;
+        sc.of(at[0], eref);
+        settle_products<8>();
+        float x[kGroups][4];
+        auto logits = [&](float ref) {
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
-                const float add = we[u] - ref;
+                const float add = sc.weights[u] - ref;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    float v = fmaf(s[nr][u][r], c[u], add);
-                    if constexpr (kMask) v = at.there[u] && kt + u * kCacheGroup + 4 * g + r < lim[nr] ? v : -INFINITY;
-                    x[nr][4 * u + r] = v;
+                    float v = fmaf(s[u][r], at[0].c[u], add);
+                    if constexpr (kMask) v = at[0].there[u] && kt + u * kCacheGroup + 4 * g + r < row.lim ? v : -INFINITY;
+                    x[u][r] = v;
                     top = fmaxf(top, v);
                 }
             }
             return top;
         };
-        float highest = -INFINITY;
+        if (__any(logits(m) > kRaise) || sc.now > eref) {
+            float top = logits(0.f);
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
+            m = now;
+            eref = __builtin_amdgcn_readfirstlane(sc.now);
+            l *= f;
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) highest = fmaxf(highest, logits(nr, m[nr]));
-        if (top_e > eref || __any(highest > kRaise)) {
-            const float unit = pow2(eref - now_e);
-            eref = now_e;
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) {
-                float top = logits(nr, 0.f);
-                top = fmaxf(top, __shfl_xor(top, 16, kWave));
-                top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float now = fmaxf(m[nr], top - kBias);
-                const float f = __builtin_amdgcn_exp2f(m[nr] - now);
-                m[nr] = now;
-                l[nr] *= f;
-#pragma unroll
-                for (int d = 0; d < kD; ++d) acc[nr][d] *= f * unit;
-                logits(nr, now);
-            }
+            for (int d = 0; d < kD; ++d) acc[d] *= fu;
+            logits(now);
         }
         if constexpr (kMask) {
-            // what lies behind the last token is not read as a value
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
-                const int left = sp.len - (kt + u * kCacheGroup + 4 * g);
-                const uint32_t keep = left <= 0 || !at.there[u] ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1u;
+                const uint32_t keep = value_mask(w.sp.len - (kt + u * kCacheGroup + 4 * g), at[0].there[u]);
 #pragma unroll
                 for (int h = 0; h < kH; ++h) {
                     vb[u][h].x &= keep;
@@ -382,137 +540,271 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                 }
             }
         }
-
 #pragma unroll
         for (int v = 0; v < kGroups / 2; ++v) {
-            typename O::vec pb[NR][kP];
+            typename O::vec pb[kP];
 #pragma unroll
-            for (int nr = 0; nr < NR; ++nr) {
+            for (int i = 0; i < 2; ++i) {
+                float *p = x[2 * v + i], sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float *w = x[nr] + 4 * (2 * v + i);
-                    float sum = 0.f;
+                for (int r = 0; r < 4; ++r) {
+                    p[r] = __builtin_amdgcn_exp2f(p[r]);
+                    sum += p[r];
+                }
+                l = fmaf(sum, sc.sums[2 * v + i], l);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        w[r] = __builtin_amdgcn_exp2f(w[r]);
-                        sum += w[r];
-                    }
-                    l[nr] = fmaf(sum, wi[2 * v + i], l[nr]);
+                for (int r = 0; r < 4; r += 2) {
+                    typename O::pair pp[kP];
+                    split<O, kP>(f32x2_t{p[r], p[r + 1]}, pp);
 #pragma unroll
-                    for (int r = 0; r < 4; r += 2) {
-                        typename O::pair p[kP];
-                        split<O, kP>(f32x2_t{w[r], w[r + 1]}, p);
-#pragma unroll
-                        for (int q = 0; q < kP; ++q) {
-                            pb[nr][q][4 * i + r] = p[q][0];
-                            pb[nr][q][4 * i + r + 1] = p[q][1];
-                        }
+                    for (int q = 0; q < kP; ++q) {
+                        pb[q][4 * i + r] = pp[q][0];
+                        pb[q][4 * i + r + 1] = pp[q][1];
                     }
                 }
             }
 #pragma unroll
             for (int d = 0; d < kD; ++d) {
                 const typename O::vec vv = from_fp8<O>(word(vb[2 * v][d >> 2], d & 3), word(vb[2 * v + 1][d >> 2], d & 3),
-                                                       va[2 * v], va[2 * v + 1]);
+                                                       sc.values[2 * v], sc.values[2 * v + 1]);
 #pragma unroll
-                for (int q = kP - 1; q >= 0; --q)
-#pragma unroll
-                    for (int nr = 0; nr < NR; ++nr) acc[nr][d] = O::mfma(vv, pb[nr][q], acc[nr][d]);
+                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma(vv, pb[q], acc[d]);
             }
         }
         fetch(a.v_cache, next, vb);
-    };
+        at[0] = next;
+        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<16>();  // (accumulators that are copied for the next tile)
+    });
 
-    // The tile of a stage, after which the stage takes the tile kStages steps on.
-    auto advance = [&](auto masked, int stage) {
-        TileAt<kGroups> next;
-        locate(kt + kStages * step, next);
-        tile(masked, ats[stage], kbs[stage], vbs[stage], next);
-        ats[stage] = next;
-        kt += step;
-    };
-    // tiles that every row sees whole, as far as all their blocks are there; then the others
-    while (kt + (kStages - 1) * step + kTile <= min(k1, all_see)) {
-        bool whole = true;
-#pragma unroll
-        for (int i = 0; i < kStages; ++i)
-#pragma unroll
-            for (int u = 0; u < kGroups; ++u) whole = whole && ats[i].there[u];
-        if (!whole) break;
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) advance(std::false_type(), i);
-    }
-    while (kt < k1) {
-#pragma unroll
-        for (int i = 0; i < kStages; ++i)
-            if (kt < k1) advance(std::true_type(), i);
-    }
-
-#pragma unroll
-    for (int nr = 0; nr < NR; ++nr) {
-        l[nr] += __shfl_xor(l[nr], 16, kWave);
-        l[nr] += __shfl_xor(l[nr], 32, kWave);
-    }
-
-    // the waves' results, 16 rows at a time: [wave][d][lane], per wave and row (reference, sum), per wave eref
+    settle_products<16>();
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
     float *stat = reinterpret_cast<float *>(lds4 + kWaves * kD * kWave);
     int *refs = reinterpret_cast<int *>(stat + kWaves * 16 * 2);
+#pragma unroll
+    for (int d = 0; d < kD; ++d) lds4[(wave * kD + d) * kWave + lane] = make_float4(acc[d][0], acc[d][1], acc[d][2], acc[d][3]);
+    if (g == 0) {
+        stat[(wave * 16 + j) * 2] = m;
+        stat[(wave * 16 + j) * 2 + 1] = l;
+    }
     if (lane == 0) refs[wave] = eref;
-    T *out = static_cast<T *>(a.out);
+    __syncthreads();
+    const Joined<kWaves> jn = join_waves<kWaves>(stat, refs, 16, j, row.padding);
 #pragma unroll
-    for (int nr = 0; nr < NR; ++nr) {
+    for (int i = 0; i < kD / kWaves; ++i) {
+        const int d = i * kWaves + wave;
+        write_row<T, DP, kWaves>(a, w, row, w.row0 + j, 16 * d + 4 * g, jn, lds4 + d * kWave + lane, kD * kWave, d == 0 && g == 0);
+    }
+}
+
+// 32 rows.  Lane (j, g) = (lane % 32, lane / 32): row j; accumulator register r of a product holds its row
+// 8 (r / 4) + 4 g + r % 4, so of a tile's 32 tokens a lane has those of the first group of 16 in registers
+// 0 .. 7 and those of the second in 8 .. 15.  As the row of V^T, lane j % 16 of half hi = j / 16 takes, of a
+// pair of 64 dims, dim 16 s + j % 16 of the hi-th for tile s (s = 0 .. 3: all of its 16-byte pieces); of a
+// last 64 dims without a pair, dim 16 (2 hi + s) + j % 16 for tile s (s = 0, 1: half of them).
+template <typename T, int DP, int kRowWaves>
+__global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1) void attend_many_kernel(AttendArgs a) {
+    typedef Operand<T> O;
+    constexpr int kTile = attend_tile(2), kGroups = 2;
+    constexpr int kStages = DP <= 128 && sizeof(T) == 2 ? 2 : 1;  // tiles in flight
+    constexpr int kC = DP / 32;                 // 16-byte loads of K per lane
+    constexpr int kPairs = DP / 128;            // pairs of 64 dims of V: a 16-byte piece per lane and four tokens
+    constexpr bool kOdd = DP % 128 != 0;        // and a last 64 dims: half a piece
+    constexpr int kD = DP / 32;                 // tiles of 32 dims
+    constexpr int kKeyWaves = kWaves / kRowWaves;  // waves that share rows
+    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes, step = kTile * kKeyWaves;
+    extern __shared__ float4 lds4[];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave % kKeyWaves, row_wave = wave / kKeyWaves;
+    const int lane = lane_id(), j = lane & 31, g = lane >> 5, i16 = lane & 15, hi = lane >> 4 & 1;
+    const int chunk = blockIdx.x % a.chunks, hk = blockIdx.x / a.chunks / a.row_blocks % a.Hkv;
+    const int kt0 = chunk * a.chunk + key_wave * kTile;
+    Walk<kGroups, DP> walk(a, blockIdx.x / a.chunks / a.row_blocks / a.Hkv, hk, step, kt0);
+    const Work w = work_of<32, kRowWaves>(a, row_wave);
+    if (a.chunks > 1 && w.k0 >= w.block_reach) return;
+
+    const Row row = row_of(a, w, w.row0 + j);
+    bf16x8_t qf[2 * kC][kQ];
+#pragma unroll
+    for (int c = 0; c < 2 * kC; ++c) load_query<T>(a, row, (c >> 1) * 32 + g * 16 + (c & 1) * 8, qf[c]);
+
+    struct Values {
+        uint4 pair[4][kPairs > 0 ? kPairs : 1];  // [tokens 8a + 4g ..][pair of 64 dims]
+        uint2 odd[4];
+    };
+    auto fetch_keys = [&](const TileAt<kGroups> &at, uint4 *to) {
+        const uint8_t *from = a.k_cache + (hi ? at.base[1] : at.base[0]) + g * 256 + i16 * 16;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) to[c] = load16(from, c * 512);
+    };
+    auto fetch_values = [&](const TileAt<kGroups> &at, Values &to) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint8_t *from = a.v_cache + at.base[q >> 1];
+#pragma unroll
+            for (int p = 0; p < kPairs; ++p)
+                to.pair[q][p] = load16(from, p * 2048 + (q & 1) * 512 + (hi * 1024 + g * 256 + i16 * 16));
+            if constexpr (kOdd)
+                to.odd[q] = *reinterpret_cast<const uint2 *>(from + kPairs * 2048 + (q & 1) * 512 + (g * 256 + i16 * 16 + hi * 8));
+        }
+    };
+    TileAt<kGroups> ats[kStages];
+    uint4 kbs[kStages][kC];
+    Values vbs[kStages];
+    if (kt0 < w.k1) {
+        walk.template begin<kStages>(kt0, w.k1, ats, [&](int i) {
+            fetch_keys(ats[i], kbs[i]);
+            fetch_values(ats[i], vbs[i]);
+        });
+    }
+    // (the queries are waited for here, not in the loop)
+#pragma unroll
+    for (int c = 0; c < 2 * kC; ++c)
+#pragma unroll
+        for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[c][q]));
+
+    f32x16_t acc[kD];
+    float m = kNothing, l = 0.f;
+    int eref = kScaleExpMin;
+#pragma unroll
+    for (int d = 0; d < kD; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+
+    walk_tiles<kTile, kStages>(kt0, step, w, ats, [&](auto masked, int stage, int kt) {
+        constexpr bool kMask = decltype(masked)::value;
+        TileAt<kGroups> &at = ats[stage], next;
+        uint4 *kb = kbs[stage];
+        Values &vb = vbs[stage];
+        walk.locate(kt + kStages * step, next);
+        f32x16_t s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2 * kC; ++c) {
+            const bf16x8_t ka = from_fp8<Operand<float>>(word(kb[c >> 1], 2 * (c & 1)), word(kb[c >> 1], 2 * (c & 1) + 1), 1.f, 1.f);
+#pragma unroll
+            for (int q = kQ - 1; q >= 0; --q) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[c][q], s, 0, 0, 0);
+        }
+        fetch_keys(next, kb);
+
+        Scales<kGroups, kP == 1> sc;
+        sc.of(at, eref);
+        settle_products<8>();
+        float x[16];
+        auto logits = [&](float ref) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u) {
+                const float add = sc.weights[u] - ref;
+#pragma unroll
+                for (int r = 8 * u; r < 8 * u + 8; ++r) {
+                    float v = fmaf(s[r], at.c[u], add);
+                    if constexpr (kMask) v = at.there[u] && kt + 8 * (r >> 2) + 4 * g + (r & 3) < row.lim ? v : -INFINITY;
+                    x[r] = v;
+                    top = fmaxf(top, v);
+                }
+            }
+            return top;
+        };
+        if (__any(logits(m) > kRaise) || sc.now > eref) {
+            float top = logits(0.f);
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
+            m = now;
+            eref = __builtin_amdgcn_readfirstlane(sc.now);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < kD; ++d) acc[d] *= fu;
+            logits(now);
+        }
+        if constexpr (kMask) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t keep = value_mask(w.sp.len - (kt + 8 * q + 4 * g), at.there[q >> 1]);
+#pragma unroll
+                for (int p = 0; p < kPairs; ++p) {
+                    vb.pair[q][p].x &= keep;
+                    vb.pair[q][p].y &= keep;
+                    vb.pair[q][p].z &= keep;
+                    vb.pair[q][p].w &= keep;
+                }
+                if constexpr (kOdd) {
+                    vb.odd[q].x &= keep;
+                    vb.odd[q].y &= keep;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            typename O::vec pb[kP];
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; r += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(x[8 * u + r]), p1 = __builtin_amdgcn_exp2f(x[8 * u + r + 1]);
+                sum += p0;
+                sum += p1;
+                typename O::pair pp[kP];
+                split<O, kP>(f32x2_t{p0, p1}, pp);
+#pragma unroll
+                for (int q = 0; q < kP; ++q) {
+                    pb[q][r] = pp[q][0];
+                    pb[q][r + 1] = pp[q][1];
+                }
+            }
+            l = fmaf(sum, sc.sums[u], l);
+#pragma unroll
+            for (int d = 0; d < kD; ++d) {
+                const int p = d >> 2, t = d & 3;
+                const bool odd = p >= kPairs;
+                const uint32_t lo = odd ? (t ? vb.odd[2 * u].y : vb.odd[2 * u].x) : word(vb.pair[2 * u][p < kPairs ? p : 0], t);
+                const uint32_t up = odd ? (t ? vb.odd[2 * u + 1].y : vb.odd[2 * u + 1].x) : word(vb.pair[2 * u + 1][p < kPairs ? p : 0], t);
+                const typename O::vec vv = from_fp8<O>(lo, up, sc.values[u], sc.values[u]);
+#pragma unroll
+                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma32(vv, pb[q], acc[d]);
+            }
+        }
+        fetch_values(next, vb);
+        at = next;
+        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<16>();
+    });
+
+    settle_products<16>();
+    l += __shfl_xor(l, 32, kWave);
+    // half of the tiles at a time: [wave][tile][register quad][lane]
+    constexpr int kHalf = kD / 2;
+    float *stat = reinterpret_cast<float *>(lds4 + kWaves * kHalf * 4 * kWave);
+    int *refs = reinterpret_cast<int *>(stat + kWaves * 32 * 2);
+    if (g == 0) {
+        stat[(wave * 32 + j) * 2] = m;
+        stat[(wave * 32 + j) * 2 + 1] = l;
+    }
+    if (lane == 0) refs[wave] = eref;
+    Joined<kKeyWaves> jn;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (half) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16_t &c = acc[half * kHalf + i];
+                lds4[((wave * kHalf + i) * 4 + q) * kWave + lane] = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
+            }
         __syncthreads();
+        if (half == 0) jn = join_waves<kKeyWaves>(stat + row_wave * kKeyWaves * 64, refs + row_wave * kKeyWaves, 32, j, row.padding);
 #pragma unroll
-        for (int d = 0; d < kD; ++d)
-            lds4[(wave * kD + d) * kWave + lane] = make_float4(acc[nr][d][0], acc[nr][d][1], acc[nr][d][2], acc[nr][d][3]);
-        if (g == 0) {
-            stat[(wave * 16 + j) * 2] = m[nr];
-            stat[(wave * 16 + j) * 2 + 1] = l[nr];
-        }
-        __syncthreads();
-        float mx = kNothing, sum = 0.f, f[kWaves];
-        int e = kScaleExpMin;
+        for (int i = 0; i < kHalf; ++i)
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            mx = fmaxf(mx, stat[(w * 16 + j) * 2]);
-            e = max(e, refs[w]);
-        }
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            f[w] = __builtin_amdgcn_exp2f(stat[(w * 16 + j) * 2] - mx);
-            sum += f[w] * stat[(w * 16 + j) * 2 + 1];
-        }
-        // a row without keys, or past new_len, is zero
-        const float inv = sum > 0.f && !padding[nr] ? 1.f / sum : 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) f[w] *= inv * pow2(refs[w] - e);
-        const float unit = pow2(e);
-#pragma unroll
-        for (int d = wave; d < kD; d += kWaves) {
-            const int dim = 16 * d + 4 * g;
-            f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float4 y = lds4[(w * kD + d) * kWave + lane];
-                o[0] += f[w] * y.x;
-                o[1] += f[w] * y.y;
-                o[2] += f[w] * y.z;
-                o[3] += f[w] * y.w;
+            for (int q = key_wave; q < 4; q += kKeyWaves) {
+                // register quad q of a tile: dims 8 (q % 2) + 4 g .. +3 of 16, of the half q / 2
+                const int d = half * kHalf + i, p = d >> 2, t = d & 3, inner = 8 * (q & 1) + 4 * g;
+                const int dim = p < kPairs ? 64 * (2 * p + (q >> 1)) + 16 * t + inner
+                                           : 128 * kPairs + 16 * (2 * (q >> 1) + t) + inner;
+                write_row<T, DP, kKeyWaves>(a, w, row, w.row0 + j, dim, jn,
+                                            lds4 + ((row_wave * kKeyWaves * kHalf + i) * 4 + q) * kWave + lane,
+                                            kHalf * 4 * kWave, d == 0 && q == 0 && g == 0);
             }
-            o *= unit;
-            if (row_at[nr] < 0) continue;
-            if (a.chunks == 1) {
-                if (dim < a.dh) store4<T>(out + row_at[nr] + dim, o);
-                continue;
-            }
-            // the chunk's result, with its reference and sum, for the joining launch
-            const int64_t part = (((int64_t)b * a.Hkv + hk) * rows + row0 + nr * 16 + j) * a.chunks + chunk;
-            store4<float>(a.part_acc + part * DP + dim, o);
-            if (d == 0 && g == 0) {
-                a.part_stat[2 * part] = mx;
-                a.part_stat[2 * part + 1] = sum;
-            }
-        }
     }
 }
 
@@ -577,25 +869,24 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a) 
     store4<T>(static_cast<T *>(a.out) + at, o * inv);
 }
 
-template <typename T, int DP, int NR>
-hipError_t launch_as(const AttendArgs &a, hipStream_t s) {
-    constexpr int kTile = attend_tile(NR);
-    const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks * a.chunks));
-    constexpr size_t lds = kWaves * (DP / 16) * kWave * 16 + kWaves * 16 * 2 * sizeof(float) + kWaves * sizeof(int);
-    if constexpr (lds > 65536) {
-        static std::atomic<uint64_t> done{0};
-        const hipError_t e = allow_large_lds(attend_kernel<T, DP, NR, kTile>, done);
+template <typename Kernel>
+hipError_t launch_attend(Kernel kernel, const AttendArgs &a, size_t lds, std::atomic<uint64_t> &done, hipStream_t s) {
+    if (lds > 65536) {
+        const hipError_t e = allow_large_lds(kernel, done);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((attend_kernel<T, DP, NR, kTile>), grid, dim3(kWaves * kWave), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks * a.chunks)), dim3(kWaves * kWave), lds, s, a);
     return hipGetLastError();
 }
 
 template <typename T, int DP>
 hipError_t launch_dp(const AttendArgs &a, hipStream_t s) {
-    if constexpr (sizeof(T) == 2 || DP <= 128)
-        if (a.row_tiles == 2) return launch_as<T, DP, 2>(a, s);
-    return launch_as<T, DP, 1>(a, s);
+    static std::atomic<uint64_t> few{0}, one{0}, two{0};
+    const size_t acc = kWaves * DP * 16 * sizeof(float), refs = kWaves * sizeof(int);
+    const size_t lds = acc + kWaves * 32 * 2 * sizeof(float) + refs;
+    if (a.row_tiles == 2 && a.row_waves == 2) return launch_attend(attend_many_kernel<T, DP, 2>, a, lds, two, s);
+    if (a.row_tiles == 2) return launch_attend(attend_many_kernel<T, DP, 1>, a, lds, one, s);
+    return launch_attend(attend_few_kernel<T, DP>, a, acc + kWaves * 16 * 2 * sizeof(float) + refs, few, s);
 }
 
 template <typename T>

@@ -60,14 +60,13 @@ struct AttendArgs {
     float *part_stat;              // [B*Hkv, rows, chunks, 2]: maximum, sum
     int B, Hq, Hkv, T, dh, block_shift, n_blocks, max_blocks, max_len, is_bf16;
     float scale;                   // times log2(e)
-    int row_tiles, row_blocks, chunk, chunks;  // attend_form
+    int row_tiles, row_waves, row_blocks, chunk, chunks;  // attend_form
 };
 constexpr int kAttendWaves = 4;
 // Keys that a wave takes at a time, by the tiles of 16 rows that it holds.
 constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
 // How a call is cut into workgroups: fills the last four fields from the others.  Up to 16 rows a
-// workgroup holds one tile of rows, above two (fp32 heads of more than 128, whose queries take three
-// planes, one).  Keys are cut into chunks until every CU has one workgroup, as long as each wave has a
+// workgroup holds one tile of 16, above two.  Keys are cut into chunks until every CU has one workgroup, as long as each wave has a
 // tile of keys; more chunks cost more in the joining launch than they bring.  GPU time, us:
 //   1 x 4 kv heads, 2304 keys: 1 chunk 13.9, 2 12.2, 3 10.4, 9 (a tile a wave) 9.7
 //   5 x 8 kv heads, 1391 keys in fp32: 1 chunk 14.3, 3 11.4, 6 10.1
@@ -75,11 +74,12 @@ constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
 //   32 x 32 kv heads, up to 3427 keys: 1 chunk 126, 2 132, 4 143
 inline void attend_form(AttendArgs &a) {
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
-    a.row_tiles = rows <= kCacheGroup || (!a.is_bf16 && a.dh > 128) ? 1 : 2;
-    const int block = kCacheGroup * a.row_tiles;
+    a.row_tiles = rows <= kCacheGroup ? 1 : 2;
+    a.row_waves = rows > 2 * kCacheGroup ? 2 : 1;
+    const int block = kCacheGroup * a.row_tiles * a.row_waves;
     a.row_blocks = (int)((rows + block - 1) / block);
     const int64_t units = (int64_t)a.B * a.Hkv * a.row_blocks;
-    const int step = attend_tile(a.row_tiles) * kAttendWaves;
+    const int step = attend_tile(a.row_tiles) * kAttendWaves / a.row_waves;
     const int64_t most = a.max_len > step ? (a.max_len + step - 1) / step : 1;
     const int64_t wanted = (256 + units - 1) / units, chunks = wanted < most ? wanted : most;
     a.chunk = (int)(((a.max_len + chunks - 1) / chunks + step - 1) / step * step);

@@ -269,7 +269,8 @@ int plan_attend(const vscan_cache_desc *d, AttendPlan *p) {
     a.scale = (d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim)) * 1.44269504088896341f;
     p->off_stat = p->bytes = 0;
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
-    if (rows >= ((int64_t)1 << 30) || (int64_t)a.B * a.Hkv * rows >= ((int64_t)1 << 31))
+    // rows, and keys a few tiles past the last one, are counted in 32 bits
+    if (rows >= ((int64_t)1 << 30) || (int64_t)a.B * a.Hkv * rows >= ((int64_t)1 << 31) || a.max_len > (1 << 30))
         return VSCAN_ERR_UNSUPPORTED;
     if (a.B == 0 || rows == 0) return VSCAN_OK;
     attend_form(a);

@@ -55,9 +55,9 @@ hipError_t launch_cache_store(const void *args, hipStream_t) {
 hipError_t launch_cache_attend(const void *args, hipStream_t) {
     const AttendArgs &a = *static_cast<const AttendArgs *>(args);
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
-    const int block = kCacheGroup * a.row_tiles;
+    const int block = kCacheGroup * a.row_tiles * a.row_waves;
     need((int64_t)a.row_blocks * block >= rows && (int64_t)(a.row_blocks - 1) * block < rows);
-    need(a.chunks >= 1 && (int64_t)a.chunk * a.chunks >= a.max_len && a.chunk % (kAttendWaves * attend_tile(a.row_tiles)) == 0);
+    need(a.chunks >= 1 && (int64_t)a.chunk * a.chunks >= a.max_len && a.chunk % (kAttendWaves / a.row_waves * attend_tile(a.row_tiles)) == 0);
     if (a.chunks > 1) {
         const size_t parts = (size_t)a.B * a.Hkv * rows * a.chunks;
         inside(a.part_acc, parts * cache_dp(a.dh) * 4);

@@ -3,7 +3,9 @@
 // A row's pair (x, y) is turned by w = position * frequency.  w is reduced to a quadrant and a rest
 // of at most pi/4 in 64 bits; sine and cosine of the rest are their Taylor sums to x^9 and x^10 in
 // 32 bits (remainders 1.8e-9 and 1.2e-10 at pi/4).  Angles depend on the token and the pair only, so
-// a thread keeps its pairs' values and walks over heads with them.
+// a thread keeps its pairs' values and walks over heads with them.  Bound: HBM, a read and a write of
+// every entry.  Angles handed around through LDS, with neighbouring heads in one workgroup, took 17.2 to
+// 20.5 us where this takes 16.9 (4352 tokens x 32 heads x 128, from the caches, before the hint below).
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -29,6 +31,10 @@ __device__ __forceinline__ void turn(int position, double freq, bool inverse, fl
     if (inverse) s = -s;
 }
 
+__device__ __forceinline__ void put16(char *p, const uint4 &v, bool stream) {
+    if (stream) store16_stream(p, v);
+    else *reinterpret_cast<uint4 *>(p) = v;
+}
 // N consecutive entries of a row: 8 or 16 bytes
 template <typename T, int N>
 struct Piece;
@@ -37,13 +43,13 @@ struct Piece<bf16_t, 8> {
     uint4 raw;
     __device__ __forceinline__ void load(const char *p) { raw = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void get(float *f) const { unpack16<bf16_t>(raw, f); }
-    __device__ __forceinline__ void store(char *p, const float *f) const {
+    __device__ __forceinline__ void store(char *p, const float *f, bool stream) const {
         union {
             __bf16 h[8];
             uint4 u;
         } o;
         for (int i = 0; i < 8; ++i) o.h[i] = (__bf16)f[i];
-        *reinterpret_cast<uint4 *>(p) = o.u;
+        put16(p, o.u, stream);
     }
 };
 template <>
@@ -56,7 +62,7 @@ struct Piece<bf16_t, 4> {
         f[2] = bf16_lo(raw.y);
         f[3] = bf16_hi(raw.y);
     }
-    __device__ __forceinline__ void store(char *p, const float *f) const {
+    __device__ __forceinline__ void store(char *p, const float *f, bool) const {
         union {
             __bf16 h[4];
             uint2 u;
@@ -70,8 +76,9 @@ struct Piece<float, 4> {
     uint4 raw;
     __device__ __forceinline__ void load(const char *p) { raw = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void get(float *f) const { unpack16<float>(raw, f); }
-    __device__ __forceinline__ void store(char *p, const float *f) const {
-        *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    __device__ __forceinline__ void store(char *p, const float *f, bool stream) const {
+        put16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])),
+              stream);
     }
 };
 
@@ -80,7 +87,7 @@ constexpr int kThreads = 256;
 // N: entries of a piece.  In halves a thread owns a piece of either half (N pairs); with adjacent
 // pairs one piece (N/2 pairs).  Pieces of the entries past rot_dim are copied where a tensor is not
 // turned in place.
-template <typename T, int N, bool ADJ>
+template <typename T, int N, bool ADJ, bool kStream>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, int rest, int per_slice) {
     const int id = blockIdx.x * kThreads + threadIdx.x;
     const int all = pieces + rest;
@@ -115,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, 
         p.load(src);
         if (!turned) {
             p.get(x);
-            p.store(dst, x);
+            p.store(dst, x, kStream);
             continue;
         }
         if constexpr (ADJ) {
@@ -125,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, 
                 y[2 * e] = x[2 * e] * c[e] - x[2 * e + 1] * sn[e];
                 y[2 * e + 1] = x[2 * e] * sn[e] + x[2 * e + 1] * c[e];
             }
-            p.store(dst, y);
+            p.store(dst, y, kStream);
         } else {
             p2.load(src + second);
             p.get(x);
@@ -136,12 +143,32 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, 
                 x[e] = u;
                 y[e] = v;
             }
-            p.store(dst, x);
-            p2.store(dst + second, y);
+            p.store(dst, x, kStream);
+            p2.store(dst + second, y, kStream);
         }
     }
 }
 
+// Whether stores carry the non-temporal hint: where more is written than the L2s hold (32 MB) and the
+// pieces of a row fill whole lines of 128 bytes.  Read from memory, without the hint and with it:
+//   4352 tokens x 32 heads x 128 in bf16: 24.0 us, 19.4 (3.7 TB/s; 15.5 us again from the caches)
+//   2 x 4096 tokens x 40 heads x 128 in bf16: 40.6 us, 32.1 (5.2 TB/s, what a copy reaches)
+//   2 x 2745 tokens x 32 heads x 80 in fp32, whose halves share lines: 25.3 us (4.4 TB/s), 29.5
+bool streams(const RopeArgs &a) {
+    const int64_t es = a.is_bf16 ? 2 : 4, run = (a.adjacent ? a.rot : a.rot / 2) * es;
+    if (run % 128 || (int64_t)a.B * a.S * (a.heads[0] + a.heads[1]) * a.rot * es < ((int64_t)32 << 20)) return false;
+    for (int i = 0; i < 2; ++i) {
+        if (!a.heads[i]) continue;
+        if (reinterpret_cast<uintptr_t>(a.out[i]) % 128) return false;
+        for (int64_t stride : a.out_stride[i])
+            if (stride * es % 128) return false;
+    }
+    return true;
+}
+
+// Heads are cut into slices until there are 1024 workgroups: fewer leave loads missing, more work out
+// angles again.  4352 tokens x 32 heads x 128 in bf16, with 256, 512, 1024, 2048 and 4096 workgroups:
+// 32.0, 21.8, 19.4, 19.6, 23.9 us.
 template <typename T, int N, bool ADJ>
 hipError_t launch(const RopeArgs &a, hipStream_t s) {
     const int pieces = ADJ ? a.rot / N : a.rot / 2 / N;
@@ -152,8 +179,11 @@ hipError_t launch(const RopeArgs &a, hipStream_t s) {
     int slices = 1;
     while (slices < heads && (int64_t)blocks * slices < 1024) slices *= 2;
     const int per = (heads + slices - 1) / slices;
-    hipLaunchKernelGGL((rope_kernel<T, N, ADJ>), dim3(blocks, (heads + per - 1) / per), dim3(kThreads), 0, s, a,
-                       pieces, rest, per);
+    const dim3 grid(blocks, (heads + per - 1) / per);
+    if (N * sizeof(T) == 16 && streams(a))
+        hipLaunchKernelGGL((rope_kernel<T, N, ADJ, N * sizeof(T) == 16>), grid, dim3(kThreads), 0, s, a, pieces, rest, per);
+    else
+        hipLaunchKernelGGL((rope_kernel<T, N, ADJ, false>), grid, dim3(kThreads), 0, s, a, pieces, rest, per);
     return hipGetLastError();
 }
 

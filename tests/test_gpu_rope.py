@@ -139,3 +139,20 @@ def test_rope_on_another_stream():
         got = vb.rope(shape, pos, freq, x["q"], x["k"])
     s.synchronize()
     assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"])
+
+
+@pytest.mark.parametrize("dtype,dh,extra", [("bf16", 128, 0), ("bf16", 128, 8), ("f32", 64, 0), ("bf16", 72, 0)])
+@pytest.mark.parametrize("pairing", [0, 1])
+def test_rope_of_more_than_the_caches_hold(dtype, dh, extra, pairing):
+    """Tens of megabytes, whole lines and parts of them, into new tensors and in place."""
+    import torch
+    B, S, Hq, Hk = 3, (36 << 20) // (3 * 32 * dh * (2 if dtype == "bf16" else 4)), 28, 4
+    shape = wl.RopeShape(dtype, B, S, Hq, Hk, dh, dh, (dh // 2,), pairing=pairing)
+    qkv = torch.randn((B, S, (Hq + Hk) * dh + extra), device="cuda").to(vb._torch_dtype(dtype))
+    rows = qkv[..., :(Hq + Hk) * dh].unflatten(2, (Hq + Hk, dh)).transpose(1, 2)
+    x = {"q": rows[:, :Hq], "k": rows[:, Hq:]}
+    _, pos, freq = _inputs(shape, 4)
+    got = vb.rope(shape, pos, freq, x["q"], x["k"])
+    _check(shape, x, pos, freq, got)
+    vb.rope(shape, pos, freq, x["q"], x["k"], in_place=True)
+    assert torch.equal(x["q"], got["q"]) and torch.equal(x["k"], got["k"])

@@ -10,11 +10,10 @@ using namespace vscan;
 
 // ---- block tables, slots and lengths -----------------------------------------------------------
 // need_b = ceil((c+n)/size) - ceil(c/size); request b's blocks start at head + sum of the needs
-// before it.  One workgroup scans the needs (the bound is its latency: a few dependent rounds of
+// before it.  A workgroup scans the needs (the bound is its latency: a few dependent rounds of
 // loads, shuffles and one barrier pair per 1024 requests); it knows whether there are blocks enough
-// only at the end, so the tables are written afterwards, from what it leaves in `requests`.
-constexpr int kPlanThreads = 1024;
-
+// only at the end, so the tables are written afterwards.  Where a launch writes them too, each of its
+// workgroups scans for itself and keeps the requests in LDS; only the first writes lengths and head.
 struct Request {
     int c, n, first;  // tokens held, tokens to come, entry of free_blocks (n < 0: nothing handed out)
 };
@@ -23,30 +22,30 @@ __device__ __forceinline__ int ceil_shift(int v, int shift) {
     return (int)(((int64_t)v + (1 << shift) - 1) >> shift);
 }
 
-// Slots of rows r, r + step, .. of request b, and its table entries.
-__device__ void write_request(const PlanArgs &a, int b, const Request &q, int r, int step) {
+// The slot of row r of request b, and the table entry of a block that it begins.
+__device__ __forceinline__ void write_row(const PlanArgs &a, int b, const Request &q, int r) {
     const int size_mask = (1 << a.block_shift) - 1;
     const int f = ceil_shift(q.c, a.block_shift);
-    int32_t *row = a.block_table + (int64_t)b * a.max_blocks;
-    for (; r < a.n_new; r += step) {
-        int slot = -1;
-        if (r < q.n) {
-            const int p = q.c + r, j = p >> a.block_shift;
-            const int block = j < f ? row[j] : a.free_blocks[q.first + j - f];
-            if (j >= f && ((p & size_mask) == 0)) row[j] = block;
-            if ((unsigned)block < (unsigned)a.n_blocks) slot = (block << a.block_shift) + (p & size_mask);
-        }
-        a.slot_map[(int64_t)b * a.n_new + r] = slot;
+    int slot = -1;
+    if (r < q.n) {
+        int32_t *row = a.block_table + (int64_t)b * a.max_blocks;
+        const int p = q.c + r, j = p >> a.block_shift;
+        const int block = j < f ? row[j] : a.free_blocks[q.first + j - f];
+        if (j >= f && ((p & size_mask) == 0)) row[j] = block;
+        if ((unsigned)block < (unsigned)a.n_blocks) slot = (block << a.block_shift) + (p & size_mask);
     }
+    a.slot_map[(int64_t)b * a.n_new + r] = slot;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a, int tables) {
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     __shared__ Request held[kPlanThreads];
     const int t = threadIdx.x;
+    const bool in_lds = tables && a.B <= kPlanThreads;
     const int cap = a.max_blocks << a.block_shift;
     const int head = min(max(*a.free_head, 0), a.n_free);
     int64_t before = 0;  // blocks of the requests of earlier rounds
+    Request own = {};
     for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
         const int b = b0 + t;
         int c = 0, n = 0;
@@ -69,38 +68,34 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a, in
             before += wave_total[w];
         }
         // an entry past the list is never used: the total is past it too then
-        const int first = (int)min((int64_t)head + mine, (int64_t)a.n_free);
-        if (b < a.B) {
-            a.requests[4 * b] = c;
-            a.requests[4 * b + 1] = n;
-            a.requests[4 * b + 2] = first;
+        own = {c, n, (int)min((int64_t)head + mine, (int64_t)a.n_free)};
+        if (!in_lds && b < a.B) {
+            a.requests[4 * b] = own.c;
+            a.requests[4 * b + 1] = own.n;
+            a.requests[4 * b + 2] = own.first;
         }
     }
     const int64_t short_by = head + before - a.n_free;
-    if (t == 0) {
-        *a.free_head_out = short_by > 0 ? head : head + (int)before;
-        *a.missing = short_by > 0 ? (int)min(short_by, (int64_t)0x7fffffff) : 0;
-    }
-    // every thread takes back what it wrote itself
-    for (int b = t; b < a.B; b += kPlanThreads) {
-        const int c = a.requests[4 * b], n = a.requests[4 * b + 1];
-        a.kv_len[b] = short_by > 0 ? c : c + n;
-        if (short_by > 0) a.requests[4 * b + 1] = -1;
+    if (blockIdx.x == 0) {
+        if (t == 0) {
+            *a.free_head_out = short_by > 0 ? head : head + (int)before;
+            *a.missing = short_by > 0 ? (int)min(short_by, (int64_t)0x7fffffff) : 0;
+        }
+        // every thread takes back what it wrote itself
+        for (int b = t; b < a.B; b += kPlanThreads) {
+            const int c = in_lds ? own.c : a.requests[4 * b], n = in_lds ? own.n : a.requests[4 * b + 1];
+            a.kv_len[b] = short_by > 0 ? c : c + n;
+            if (!in_lds && short_by > 0) a.requests[4 * b + 1] = -1;
+        }
     }
     if (!tables) return;
-    // threads of a request: as many as it has rows, up to what a round over all requests leaves
-    int each = 1;
-    while (each < a.n_new && each * 2 * min(a.B, kPlanThreads) <= kPlanThreads) each *= 2;
-    const int at_once = kPlanThreads / each;
-    for (int b0 = 0; b0 < a.B; b0 += at_once) {
-        __syncthreads();
-        // request b was written by thread b % kPlanThreads
-        const int own = (t - b0) & (kPlanThreads - 1), mine = b0 + own;
-        if (own < at_once && mine < a.B)
-            held[own] = {a.requests[4 * mine], a.requests[4 * mine + 1], a.requests[4 * mine + 2]};
-        __syncthreads();
-        const int i = t / each, b = b0 + i;
-        if (b < a.B) write_request(a, b, held[i], t % each, each);
+    held[t] = {own.c, short_by > 0 ? -1 : own.n, own.first};
+    __syncthreads();
+    const uint32_t rows = (uint32_t)a.B * a.n_new;
+    for (uint32_t i = blockIdx.x * kPlanThreads + t; i < rows; i += gridDim.x * kPlanThreads) {
+        const int b = i / (uint32_t)a.n_new;
+        const Request q = in_lds ? held[b] : Request{a.requests[4 * b], a.requests[4 * b + 1], a.requests[4 * b + 2]};
+        write_row(a, b, q, i - (uint32_t)b * a.n_new);
     }
 }
 
@@ -108,7 +103,7 @@ constexpr int kTableThreads = 256;
 __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(PlanArgs a, int row_parts) {
     const int b = blockIdx.x / row_parts, part = blockIdx.x % row_parts;
     const Request q = {a.requests[4 * b], a.requests[4 * b + 1], a.requests[4 * b + 2]};
-    write_request(a, b, q, part * kTableThreads + threadIdx.x, row_parts * kTableThreads);
+    for (int r = part * kTableThreads + threadIdx.x; r < a.n_new; r += row_parts * kTableThreads) write_row(a, b, q, r);
 }
 
 // ---- new keys and values -----------------------------------------------------------------------
@@ -397,6 +392,10 @@ hipError_t launch_store_as(const StoreArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// A page is a wave's work up to 32 tokens: 32 sequences x 8 kv heads x 128 in bf16, GPU time in us of a wave
+// and of a workgroup: 1267 tokens in blocks of 32 45.1 and 50.6, of 64 46.1 and 41.4, of 128 59.6 and 47.4;
+// one token 4.1 and 4.8 in either, but a wave takes long to fill or rescale a large page.  A lane that can
+// meet one unit only holds one: 1267 tokens in blocks of 16 40.7, where lanes with room for four take 51.
 template <typename T, int DP>
 hipError_t launch_store_dp(const StoreArgs &a, hipStream_t s) {
     constexpr int kMost = sizeof(T) == 2 ? 4 : 2;  // 64 registers
@@ -425,7 +424,8 @@ namespace vscan {
 
 hipError_t launch_cache_plan(const void *args, hipStream_t s) {
     const PlanArgs &a = *static_cast<const PlanArgs *>(args);
-    hipLaunchKernelGGL(cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, plan_in_one(a) ? 1 : 0);
+    const int workgroups = plan_workgroups(a);
+    hipLaunchKernelGGL(cache_plan_kernel, dim3(workgroups ? workgroups : 1), dim3(kPlanThreads), 0, s, a, workgroups > 0);
     return hipGetLastError();
 }
 

@@ -212,7 +212,7 @@ int cache_plan(const vscan_cache_desc *d, const int32_t *cached_len, const int32
     a.n_free = n_free;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const int rc2 = enqueue("cache_plan", s, launch_cache_plan, &a);
-    if (rc2 != VSCAN_OK || plan_in_one(a)) return rc2;
+    if (rc2 != VSCAN_OK || plan_workgroups(a)) return rc2;
     return enqueue("cache_tables", s, launch_cache_tables, &a);
 }
 

@@ -71,6 +71,22 @@ def test_plan_without_enough_blocks_hands_out_nothing(B, n_new):
     assert int(got["missing"]) >= 1
 
 
+@pytest.mark.parametrize("B,n_new", [(1024, 1), (1024, 5), (1025, 5), (300, 40), (4, 9000), (2000, 2), (1, 300000)])
+@pytest.mark.parametrize("missing", [0, 1])
+def test_plan_in_place_and_beside(B, n_new, missing):
+    """The lengths and the head overwritten, one of them, and neither: one result."""
+    shape, cached, new, free, head, table = _plan_case(B, n_new, 16, -(-n_new // 16) + 3, seed=B + n_new, spare=0)
+    free = free[:len(free) - missing]
+    for over in ((), ("kv_len",), ("free_head",), ("kv_len", "free_head")):
+        c, h, t = _i32(cached), _i32([head]), _i32(table).view(B, -1)
+        got = vb.cache_plan(shape, c, _i32(new), _i32(free), h, t, out={n: {"kv_len": c, "free_head": h}[n] for n in over})
+        want = ref.plan(shape, cached, new, free, head, table)
+        assert got["kv_len"].tolist() == want[2] and (int(got["free_head"]), int(got["missing"])) == want[3:]
+        assert got["slot_map"].tolist() == want[1] and t.tolist() == want[0]
+        assert c.tolist() == (want[2] if "kv_len" in over else cached)
+        assert int(h) == (want[3] if "free_head" in over else head)
+
+
 def test_plan_holds_lengths_and_blocks_inside_their_ranges():
     shape = wl.CacheShape("bf16", 6, 1, 1, 64, 16, 40, 4, 20)
     table = [[i * 4 + j for j in range(4)] for i in range(6)]

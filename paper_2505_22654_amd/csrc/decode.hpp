@@ -75,23 +75,35 @@ struct AttendArgs {
 constexpr int kAttendWaves = 4;
 // Keys that a wave takes at a time, by the tiles of 16 rows that it holds.
 constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
-// How a call is cut into workgroups: fills the last four fields from the others.  Up to 16 rows a
-// workgroup holds one tile of 16, above two.  Keys are cut into chunks until every CU has one workgroup, as long as each wave has a
-// tile of keys; more chunks cost more in the joining launch than they bring.  GPU time, us:
+// How a call is cut into workgroups: fills the last five fields from the others.
+// A workgroup of the few-row kernel holds one tile of 16 rows, of the many-row kernel 32 rows a wave.  16
+// heads of 8 kv heads, 3000 keys, GPU time in us, few and many: 8 rows 19.8 and 20.7, 16 rows 19.6 and
+// 20.3, 20 rows (two tiles of 16) 21.7 and 20.6, 32 rows 25.5 and 22.5.
+// Two of the many-row kernel's waves share their keys, each with rows of its own, where that leaves a
+// workgroup a CU: keys are read half as often, but walked by half the waves.  One and two row waves, by
+// the workgroups that two make:
+//   1 x 4 kv heads, 63 rows, 2304 keys (4): 13.3, 17.7     4 x 4, 63 rows, 30000 keys (16): 33, 35.6
+//   16 x 8, 36 rows, 3000 keys (128): 24.5, 28             16 x 8, 64 rows (128): 30.2, 30.2
+//   64 x 4, 49 rows, 3000 keys (256): 47, 39               16 x 8, 192 rows (384): 69, 56.6
+//   64 x 8, 64 rows, 3000 keys (512): 92, 75               64 x 8, 80 rows (1024): 114, 117
+// Keys are cut into chunks until every CU has one workgroup, as long as each wave has a tile of keys; more
+// chunks cost more in the joining launch than they bring:
 //   1 x 4 kv heads, 2304 keys: 1 chunk 13.9, 2 12.2, 3 10.4, 9 (a tile a wave) 9.7
 //   5 x 8 kv heads, 1391 keys in fp32: 1 chunk 14.3, 3 11.4, 6 10.1
 //   4 x 4 kv heads, up to 65536 keys: 8 chunks 46.1, 16 44.2, 32 44.2, 64 60.8, 128 85
 //   32 x 32 kv heads, up to 3427 keys: 1 chunk 126, 2 132, 4 143
 inline void attend_form(AttendArgs &a) {
-    const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
+    constexpr int64_t kCus = 256;
+    const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T, heads = (int64_t)a.B * a.Hkv;
+    const int64_t pair = 4 * kCacheGroup;  // rows of two row waves
     a.row_tiles = rows <= kCacheGroup ? 1 : 2;
-    a.row_waves = rows > 2 * kCacheGroup ? 2 : 1;
+    a.row_waves = rows > 2 * kCacheGroup && heads * ((rows + pair - 1) / pair) >= kCus ? 2 : 1;
     const int block = kCacheGroup * a.row_tiles * a.row_waves;
     a.row_blocks = (int)((rows + block - 1) / block);
-    const int64_t units = (int64_t)a.B * a.Hkv * a.row_blocks;
+    const int64_t units = heads * a.row_blocks;
     const int step = attend_tile(a.row_tiles) * kAttendWaves / a.row_waves;
     const int64_t most = a.max_len > step ? (a.max_len + step - 1) / step : 1;
-    const int64_t wanted = (256 + units - 1) / units, chunks = wanted < most ? wanted : most;
+    const int64_t wanted = (kCus + units - 1) / units, chunks = wanted < most ? wanted : most;
     a.chunk = (int)(((a.max_len + chunks - 1) / chunks + step - 1) / step * step);
     if (a.chunk < step) a.chunk = step;
     a.chunks = a.max_len > a.chunk ? (a.max_len + a.chunk - 1) / a.chunk : 1;

@@ -202,14 +202,14 @@ struct Rows {
         for (int i = 0; i < kLoads; ++i) unpack16<T>(raw[j][i], f + i * ElemTraits<T>::kPer16B);
     }
     // rows from n on were read before it was known that they go elsewhere
-    __device__ __forceinline__ float largest(int row, int n) const {
+    __device__ __forceinline__ float largest(int row, int n, bool finite) const {
         float m = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float f[8], r = 0.f;
             get(j, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r = fmaxf(r, fabsf(f[e]));
+            for (int e = 0; e < 8; ++e) r = fmaxf(r, finite && fabsf(f[e]) == INFINITY ? 0.f : fabsf(f[e]));
             m = row + j < n ? fmaxf(m, r) : m;
         }
         return m;
@@ -297,20 +297,25 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(StoreArgs a,
         __syncthreads();
         n = first_bad;
     }
-    float amax = 0.f;
+    // (fmaxf passes NaN over)
+    auto largest = [&](bool finite) {
+        float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < kHold; ++i) {
-        const int u = lane + i * LANES;
-        if (u < units) amax = fmaxf(amax, held[i].largest(unit_at<DP>(q0 * (DP / 8) + u, kind).token - at0, n));
-    }
-    for (int u = lane + kHold * LANES; u < units; u += LANES) {
-        const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
-        Rows<T> rows;
-        rows.load(src, un.token - at0, n, un.dim, a.dh);
-        amax = fmaxf(amax, rows.largest(un.token - at0, n));
-    }
-    amax = wave_max(amax);
-    if constexpr (LANES > kWave) amax = block_max(amax, red);
+        for (int i = 0; i < kHold; ++i) {
+            const int u = lane + i * LANES;
+            if (u < units) m = fmaxf(m, held[i].largest(unit_at<DP>(q0 * (DP / 8) + u, kind).token - at0, n, finite));
+        }
+        for (int u = lane + kHold * LANES; u < units; u += LANES) {
+            const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
+            Rows<T> rows;
+            rows.load(src, un.token - at0, n, un.dim, a.dh);
+            m = fmaxf(m, rows.largest(un.token - at0, n, finite));
+        }
+        if constexpr (LANES > kWave) return block_max(m, red);
+        else return wave_max(m);
+    };
+    float amax = largest(false);
+    if (amax == INFINITY) amax = largest(true);
 
     const bool begun = at0 == 0;
     float *scale = a.scale[kind] + page;

@@ -197,6 +197,32 @@ def test_store_of_zeros_extremes_and_ties():
         _check_store(shape, cache, torch.full_like(k, x), torch.full_like(k, -x), slots)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("block,n_new,cached", [(16, 1, 3), (16, 40, 5), (64, 100, 0), (256, 300, 9)])
+def test_store_holds_infinities_and_nan_as_nan(dtype, block, n_new, cached):
+    """They leave the scale and their neighbours alone."""
+    import torch
+    shape = wl.CacheShape(dtype, 1, 2, 2, 72, block, 30, 30, n_new)
+    g = torch.Generator(device="cuda").manual_seed(block)
+    k, v = (torch.randn((1, 2, n_new, 72), generator=g, device="cuda").to(vb._torch_dtype(dtype)) for _ in "kv")
+    odd = torch.rand(k.shape, generator=g, device="cuda") < 0.02
+    odd[0, 0, 0, 7] = odd[0, 1, -1, 71] = True
+    odd[0, 1, 0, :] = True                                       # a row of nothing else
+    bad = torch.tensor([float("inf"), -float("inf"), float("nan")], device="cuda").to(k.dtype)
+    bad = bad[torch.arange(k.numel(), device="cuda").view(k.shape) % 3]
+    slots = _i32(_slots(shape, [cached], [n_new], 3))
+    plain, got = _fresh_cache(shape, 1), _fresh_cache(shape, 1)
+    vb.cache_store(shape, torch.where(odd, 0, k), torch.where(odd, 0, v), slots, plain)
+    vb.cache_store(shape, torch.where(odd, bad, k), torch.where(odd, bad, v), slots, got)
+    for n in "kv":
+        assert torch.equal(plain[n + "_scale"], got[n + "_scale"])
+        a, b = ref.read(plain, shape, n), ref.read(got, shape, n)
+        want = torch.zeros(a.shape, dtype=torch.bool, device="cuda")
+        for r, s in enumerate(slots[0].tolist()):
+            want[s // block, :, s % block, :72] = odd[0, :, r]
+        assert torch.equal(b.isnan(), want) and torch.equal(a[~want], b[~want])
+
+
 def test_store_leaves_out_rows_it_cannot_place():
     """-1, slots outside the cache, rows that do not continue their block; other blocks stay."""
     import torch

@@ -462,6 +462,7 @@ int vscan_cache_plan(const vscan_cache_desc *desc, const int32_t *cached_len,
  *   - A block whose offset 0 is among the new tokens is begun: its scale is the
  *     least power of two s with |x| <= 448 s for all of them (2^-120 .. 2^120), the
  *     values are x/s rounded to nearest even, and the rest of the block is zero.
+ *     Infinities and NaN do not count for the scale and are held as NaN.
  *   - In a block that is continued the scale only grows: where the new tokens need
  *     a larger one, the values before them are scaled down to it (exact, as scales
  *     are powers of two, but for values that become subnormal).
@@ -482,8 +483,9 @@ int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v
  *   new_len     DEVICE [B] (held inside 0 .. n_new), or NULL: n_new everywhere
  *   out         DEVICE [B, Hq, n_new, dh]; rows t >= new_len[b], and rows that see
  *               no key, are zero
- * A block number outside the cache stands for keys that are not there.  Logits,
- * softmax and sums are in 32 bits.  Workspace: vscan_cache_attend_workspace_size
+ * A block number outside the cache stands for keys that are not there.  NaN in a
+ * key or a value reaches the rows that see it and no others.  out must not overlap
+ * an input.  Logits, softmax and sums are in 32 bits.  Workspace: vscan_cache_attend_workspace_size
  * bytes, 16-byte aligned (0: none is needed, NULL is taken). */
 int vscan_cache_attend_workspace_size(const vscan_cache_desc *desc, size_t *bytes);
 int vscan_cache_attend(const vscan_cache_desc *desc, const void *q, const void *k_cache,

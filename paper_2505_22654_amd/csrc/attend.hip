@@ -23,6 +23,7 @@
 // sequences and rows leave compute units idle the keys are cut into chunks over workgroups, which a
 // second launch joins.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
@@ -209,7 +210,7 @@ __device__ __forceinline__ Row row_of(const AttendArgs &a, const Work &w, int r)
 // Eight entries of a query as planes.
 template <typename T>
 __device__ __forceinline__ void load_query(const AttendArgs &a, const Row &row, int d, bf16x8_t *out) {
-    const bool ok = row.at >= 0 && d < a.dh;
+    const bool ok = row.at >= 0 && !row.padding && d < a.dh;
     const T *src = static_cast<const T *>(a.q) + max(row.at, (int64_t)0);
     if constexpr (sizeof(T) == 2) {
         union {
@@ -280,6 +281,16 @@ struct Walk {
         lane_c *= a.scale;
         lane_e = lane_block >= 0 ? exp_of(__int_as_float(lane_e)) : kScaleExpMin;
         asm volatile("" ::"v"(block_ahead));
+    }
+    // Where the tile at key kt lies, from the table.
+    __device__ __forceinline__ void look_up(int kt, TileAt<kGroups> &at) const {
+        const int size = 1 << a.block_shift;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            const int key = kt + u * kCacheGroup, block = key < k1 ? table[key >> a.block_shift] : -1;
+            at.there[u] = (unsigned)block < (unsigned)a.n_blocks;
+            at.base[u] = (((int64_t)(at.there[u] ? block : 0) * a.Hkv + hk) * size + (key & (size - 1))) * DP;
+        }
     }
     // Where the next tile lies, at key kt (what is not there is read from the first page: no load depends
     // on a branch).
@@ -371,6 +382,32 @@ __device__ __forceinline__ uint32_t value_mask(int left, bool there) {
     return left <= 0 || !there ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1u;
 }
 
+// NaN bytes of four e4m3 values: as 0xff.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+    const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return (top >> 7) * 255u;
+}
+__device__ __forceinline__ uint32_t take_nan(uint32_t &w) {
+    const uint32_t n = nan_bytes(w);
+    w &= ~n;
+    return n;
+}
+// A weight of 0 does not keep a NaN out of a sum.  So the masked tiles, where some rows do not see a key,
+// leave NaN out, and a wave that has met any goes over those tiles once more at its end: ones where a value is
+// NaN times ones where a row sees its key count what makes a sum NaN.
+template <typename O>
+__device__ __forceinline__ typename O::vec ones_at(uint32_t lo, uint32_t hi) {
+    return from_fp8<O>(nan_bytes(lo) & 0x38383838u, nan_bytes(hi) & 0x38383838u, 1.f, 1.f);  // 0x38: 1.0
+}
+// .. of the eight keys lo .. lo + 3 and hi .. hi + 3
+template <typename O>
+__device__ __forceinline__ typename O::vec seen_keys(int lo, int hi, int lim) {
+    typename O::vec r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (e < 4 ? lo + e : hi + e - 4) < lim ? 1.f : 0.f;
+    return r;
+}
+
 // The results of the waves of a workgroup for a lane's row, from (reference, sum) pairs and scale
 // references in LDS: factors of their accumulators, and what the row has in all.
 template <int kN>
@@ -414,6 +451,7 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, const Work &w, co
         o[3] += jn.f[v] * y.w;
     }
     o *= jn.unit;
+    if (row.padding) o = f32x4_t{0.f, 0.f, 0.f, 0.f};  // (a NaN of a value would stay one under a factor of 0)
     if (row.at < 0) return;
     if (a.chunks == 1) {
         if (dim < a.dh) store4<T>(static_cast<T *>(a.out) + row.at + dim, o);
@@ -476,6 +514,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     f32x4_t acc[kD];
     float m = kNothing, l = 0.f;
     int eref = kScaleExpMin;  // acc holds sums in units of 2^eref
+    int nan_from = INT_MAX;   // the first masked tile with a NaN
 #pragma unroll
     for (int d = 0; d < kD; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
@@ -539,6 +578,12 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                     vb[u][h].w &= keep;
                 }
             }
+            uint32_t nan = 0;
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                for (int h = 0; h < kH; ++h) nan |= take_nan(vb[u][h].x) | take_nan(vb[u][h].y) | take_nan(vb[u][h].z) | take_nan(vb[u][h].w);
+            if (__any(nan)) nan_from = min(nan_from, kt);
         }
 #pragma unroll
         for (int v = 0; v < kGroups / 2; ++v) {
@@ -577,6 +622,26 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     });
 
     settle_products<16>();
+    if (nan_from < w.k1) {
+        for (int kt = nan_from; kt < w.k1; kt += step) {
+            TileAt<kGroups> t;
+            walk.look_up(kt, t);
+            fetch(a.v_cache, t, vb);
+#pragma unroll
+            for (int v = 0; v < kGroups / 2; ++v) {
+                const int lo = kt + 2 * v * kCacheGroup + 4 * g, up = lo + kCacheGroup;
+                const typename O::vec seen = seen_keys<O>(t.there[2 * v] ? lo : INT_MAX - 4, t.there[2 * v + 1] ? up : INT_MAX - 4, row.lim);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    const uint32_t w0 = word(vb[2 * v][d >> 2], d & 3), w1 = word(vb[2 * v + 1][d >> 2], d & 3);
+                    const f32x4_t count = O::mfma(ones_at<O>(w0, w1), seen, f32x4_t{0.f, 0.f, 0.f, 0.f});
+                    settle_products<8>();
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[d][r] = count[r] > 0.f ? NAN : acc[d][r];
+                }
+            }
+        }
+    }
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
     float *stat = reinterpret_cast<float *>(lds4 + kWaves * kD * kWave);
@@ -648,6 +713,13 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                 to.odd[q] = *reinterpret_cast<const uint2 *>(from + kPairs * 2048 + (q & 1) * 512 + (g * 256 + i16 * 16 + hi * 8));
         }
     };
+    // a lane's part of the u-th 16 tokens as rows of V^T tile d
+    auto value_words = [](const Values &vb, int u, int d, uint32_t &lo, uint32_t &up) {
+        const int p = d >> 2, t = d & 3;
+        const bool odd = p >= kPairs;
+        lo = odd ? (t ? vb.odd[2 * u].y : vb.odd[2 * u].x) : word(vb.pair[2 * u][p < kPairs ? p : 0], t);
+        up = odd ? (t ? vb.odd[2 * u + 1].y : vb.odd[2 * u + 1].x) : word(vb.pair[2 * u + 1][p < kPairs ? p : 0], t);
+    };
     TileAt<kGroups> ats[kStages];
     uint4 kbs[kStages][kC];
     Values vbs[kStages];
@@ -665,7 +737,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 
     f32x16_t acc[kD];
     float m = kNothing, l = 0.f;
-    int eref = kScaleExpMin;
+    int eref = kScaleExpMin, nan_from = INT_MAX;
 #pragma unroll
     for (int d = 0; d < kD; ++d)
 #pragma unroll
@@ -734,6 +806,15 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                     vb.odd[q].y &= keep;
                 }
             }
+            uint32_t nan = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int p = 0; p < kPairs; ++p)
+                    nan |= take_nan(vb.pair[q][p].x) | take_nan(vb.pair[q][p].y) | take_nan(vb.pair[q][p].z) | take_nan(vb.pair[q][p].w);
+                if constexpr (kOdd) nan |= take_nan(vb.odd[q].x) | take_nan(vb.odd[q].y);
+            }
+            if (__any(nan)) nan_from = min(nan_from, kt);
         }
 #pragma unroll
         for (int u = 0; u < kGroups; ++u) {
@@ -755,10 +836,8 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             l = fmaf(sum, sc.sums[u], l);
 #pragma unroll
             for (int d = 0; d < kD; ++d) {
-                const int p = d >> 2, t = d & 3;
-                const bool odd = p >= kPairs;
-                const uint32_t lo = odd ? (t ? vb.odd[2 * u].y : vb.odd[2 * u].x) : word(vb.pair[2 * u][p < kPairs ? p : 0], t);
-                const uint32_t up = odd ? (t ? vb.odd[2 * u + 1].y : vb.odd[2 * u + 1].x) : word(vb.pair[2 * u + 1][p < kPairs ? p : 0], t);
+                uint32_t lo, up;
+                value_words(vb, u, d, lo, up);
                 const typename O::vec vv = from_fp8<O>(lo, up, sc.values[u], sc.values[u]);
 #pragma unroll
                 for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma32(vv, pb[q], acc[d]);
@@ -770,6 +849,31 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     });
 
     settle_products<16>();
+    if (nan_from < w.k1) {
+        for (int kt = nan_from; kt < w.k1; kt += step) {
+            TileAt<kGroups> at;
+            Values vb;
+            walk.look_up(kt, at);
+            fetch_values(at, vb);
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u) {
+                const int lo = at.there[u] ? kt + u * kCacheGroup + 4 * g : INT_MAX - 12;
+                const typename O::vec seen = seen_keys<O>(lo, lo + 8, row.lim);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    uint32_t w0, w1;
+                    value_words(vb, u, d, w0, w1);
+                    f32x16_t count;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) count[r] = 0.f;
+                    count = O::mfma32(ones_at<O>(w0, w1), seen, count);
+                    settle_products<16>();
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[d][r] = count[r] > 0.f ? NAN : acc[d][r];
+                }
+            }
+        }
+    }
     l += __shfl_xor(l, 32, kWave);
     // half of the tiles at a time: [wave][tile][register quad][lane]
     constexpr int kHalf = kD / 2;

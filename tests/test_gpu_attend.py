@@ -214,3 +214,95 @@ def test_results_do_not_depend_on_the_run():
     first = vb.cache_attend(shape, q, cache, table, kv)["out"]
     for _ in range(3):
         assert torch.equal(vb.cache_attend(shape, q, cache, table, kv)["out"], first)
+
+
+def _poison(shape, cache, rows, table, name, b, j, head, dim):
+    """Makes dim `dim` of token j of sequence b a NaN in the cache, and 0 in the rows of the definition."""
+    bs, dp = shape.block_size, (shape.head_dim + 63) // 64 * 64
+    block = int(table[b, j // bs])
+    flat = cache[name].view(shape.n_blocks, shape.kv_heads, -1)
+    flat[block, head, ref.offset(name, j % bs, dim, dp)] = 0xff if j % 2 else 0x7f
+    rows[name][block, head, j % bs, dim] = 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,dh,block,T,lens", [
+    (4, 4, 128, 16, 5, [40, 5, 3000]), (8, 2, 64, 32, 4, [64, 3]), (6, 2, 128, 16, 70, [70, 400, 33]),
+    (2, 1, 192, 64, 40, [41, 300]), (4, 2, 256, 16, 9, [9, 129]), (14, 2, 80, 16, 300, [300, 1200]), (32, 8, 128, 16, 64, [500] * 40)])
+def test_nan_reaches_the_rows_that_see_it(dtype, hq, hkv, dh, block, T, lens):
+    """NaN in values and keys of the new tokens and before: rows that stand before them, and other heads and
+    sequences, do not have any; dims whose values are whole neither, where the keys are."""
+    import torch
+    blocks = sum(-(-n // block) for n in lens) + 3
+    shape = wl.CacheShape(dtype, len(lens), hq, hkv, dh, block, blocks, max(-(-n // block) for n in lens), T)
+    q, cache, table, rows = make(shape, lens, 77)
+    want_nan = torch.zeros(q.shape, dtype=torch.bool, device="cuda")
+    G, rng = hq // hkv, np.random.default_rng(5)
+    places = [(0, lens[0] - 1, 0, 0, "v"), (0, max(lens[0] - T, 0), hkv - 1, dh - 1, "v"), (1, lens[1] - 1, 0, dh // 2, "k")]
+    for b, n in enumerate(lens):
+        first = max(n - T, 0)
+        places += [(b, int(rng.integers(first, n)), int(rng.integers(hkv)), int(rng.integers(dh)), "v") for _ in range(6)]
+    if lens[-1] > 2 * T:
+        places.append((len(lens) - 1, lens[-1] - T - 1, 0, 1, "v"))  # a token that every row sees
+    for b, j, h, d, name in places:
+        _poison(shape, cache, rows, table, name, b, j, h, d)
+        t0 = max(j - (lens[b] - T), 0)
+        want_nan[b, h * G:(h + 1) * G, t0:, slice(None) if name == "k" else d] = True
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    want, bound = ref.attend(shape, q, rows["k"], rows["v"], cache["v_scale"], table, lens, None)
+    keyed = want_nan.all(-1, keepdim=True)
+    assert torch.equal(got.isnan(), want_nan)
+    over = (got.double() - want).abs() - bound - HALF_STEP[dtype] * want.abs()
+    assert float(over[~want_nan & ~keyed].max()) <= 0
+
+
+@pytest.mark.parametrize("T,lens", [(4, [30, 9, 2]), (70, [100, 70, 40]), (3, [5000, 4000, 1])])
+def test_padding_rows_are_zero_whatever_they_hold(T, lens):
+    import torch
+    for dtype in ("bf16", "f32"):
+        shape = wl.CacheShape(dtype, 3, 8, 2, 64, 16, sum(-(-n // 16) for n in lens) + 2, -(-max(lens) // 16), T)
+        q, cache, table, rows = make(shape, lens, 12)
+        new = [T - 1, 1, 0]
+        for b, n in enumerate(new):
+            q[b, :, n:] = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device="cuda").to(q.dtype).repeat(16)
+        got, _ = check(shape, torch.where(torch.isfinite(q) & (q.abs() < 1e38), q, 0), cache, table, rows, lens, new)
+        again = vb.cache_attend(shape, q, cache, table, i32(lens), i32(new))["out"]
+        assert torch.equal(got, again)
+        for b, n in enumerate(new):
+            assert not again[b, :, n:].any()
+
+
+def test_two_calls_at_once_and_two_graphs():
+    """Calls on two streams, eager and captured, each with its own workspace, and one workspace for calls
+    that follow each other."""
+    import torch
+    shapes, states, want = [], [], []
+    for i, (hq, hkv, dh, T, lens) in enumerate([(28, 4, 128, 1, [3000, 7, 2100]), (8, 2, 64, 50, [900, 60, 333])]):
+        shapes.append(wl.CacheShape("bf16", 3, hq, hkv, dh, 16, sum(-(-n // 16) for n in lens) + 3, -(-max(lens) // 16), T))
+        q, cache, table, rows = make(shapes[i], lens, 40 + i)
+        states.append((q, cache, table, i32(lens)))
+        want.append(check(shapes[i], q, cache, table, rows, lens, None)[0])
+    streams = [torch.cuda.Stream() for _ in shapes]
+    graphs, outs = [], []
+    torch.cuda.synchronize()
+    for sh, st, stream in zip(shapes, states, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            outs.append(vb.cache_attend(sh, *st)["out"])
+        graphs.append(g)
+    for _ in range(5):
+        eager = []
+        for i, stream in enumerate(streams):
+            outs[i].fill_(-1)
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                graphs[i].replay()
+                eager.append(vb.cache_attend(shapes[1 - i], *states[1 - i])["out"])
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(outs[i], want[i]) and torch.equal(eager[i], want[1 - i])
+    need = max(vb.cache_attend_workspace_size(vb.cache_desc(sh)) for sh in shapes)
+    space = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    for i in (0, 1, 0):
+        got = vb.cache_attend(shapes[i], *states[i], workspace=space)["out"]
+        assert torch.equal(got, want[i])

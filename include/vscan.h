@@ -470,7 +470,9 @@ int vscan_cache_plan(const vscan_cache_desc *desc, const int32_t *cached_len,
  * offset of row 0's slot (0 where that is negative), and the rows of one block
  * follow each other in it.  A row whose slot says otherwise, or whose block's first
  * row here or a row between does, is left out, and so are slots outside the cache.
- * No two sequences may share a block that is written. */
+ * No two sequences may share a block that is written.  VSCAN_ERR_UNSUPPORTED where
+ * 2 B Hkv times the blocks that n_new rows can touch reach 2^24 (2^26 for blocks of
+ * 16 and 32). */
 int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v,
                       const int32_t *slot_map, void *k_cache, void *v_cache, float *k_scale,
                       float *v_scale, void *stream);

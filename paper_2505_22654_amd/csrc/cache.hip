@@ -407,7 +407,7 @@ hipError_t launch_store_dp(const StoreArgs &a, hipStream_t s) {
     const int size = 1 << a.block_shift;
     // quads that one call's rows can lie in
     const int units = min(size / 4, (a.n_new + 6) / 4) * (DP / 8);
-    if (size <= 32)
+    if (store_pages(size) > 1)
         return units <= kWave ? launch_store_as<T, DP, kWave, 1>(a, s) : launch_store_as<T, DP, kWave, kMost>(a, s);
     return units <= kStoreThreads ? launch_store_as<T, DP, kStoreThreads, 1>(a, s)
                                   : launch_store_as<T, DP, kStoreThreads, kMost>(a, s);

@@ -58,6 +58,8 @@ struct StoreArgs {
     const int32_t *slot_map;
     int B, Hkv, n_new, seq_len, dh, block_shift, n_blocks, is_bf16;
 };
+// Pages (a block's part of one kv head, of k or of v) of a workgroup: a wave or all of it each.
+constexpr int store_pages(int block_size) { return block_size <= 32 ? 4 : 1; }
 hipError_t launch_cache_store(const void *args, hipStream_t s);
 
 struct AttendArgs {

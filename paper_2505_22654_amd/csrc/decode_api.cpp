@@ -15,6 +15,7 @@ namespace {
 using namespace vscan;
 
 constexpr size_t kAlign = 256;
+constexpr int64_t kMaxWorkgroups = (int64_t)1 << 24;  // of 256 threads: a grid has less than 2^32 threads
 inline size_t align_up(size_t v) { return (v + kAlign - 1) & ~(kAlign - 1); }
 inline bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline int elem_bytes(int dtype) { return dtype == VSCAN_BF16 ? 2 : 4; }
@@ -220,9 +221,9 @@ int cache_store(const vscan_cache_desc *d, const void *k, const void *v, const i
                 void *k_cache, void *v_cache, float *k_scale, float *v_scale, void *stream) {
     const int rc = check_cache(d);
     if (rc != VSCAN_OK) return rc;
-    // one workgroup per (k or v, sequence, kv head, block that the new rows touch)
+    // one wave or workgroup per (k or v, sequence, kv head, block that the new rows touch)
     const int64_t runs = (d->n_new + d->block_size - 2) / d->block_size + 1;
-    if ((int64_t)d->batch * d->kv_heads * runs * 2 >= ((int64_t)1 << 31)) return VSCAN_ERR_UNSUPPORTED;
+    if ((int64_t)d->batch * d->kv_heads * runs * 2 >= kMaxWorkgroups * store_pages(d->block_size)) return VSCAN_ERR_UNSUPPORTED;
     if (d->batch == 0 || d->n_new == 0) return VSCAN_OK;
     if (!k || !v || !slot_map || !k_cache || !v_cache || !k_scale || !v_scale) return VSCAN_ERR_NULL;
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
@@ -274,7 +275,7 @@ int plan_attend(const vscan_cache_desc *d, AttendPlan *p) {
         return VSCAN_ERR_UNSUPPORTED;
     if (a.B == 0 || rows == 0) return VSCAN_OK;
     attend_form(a);
-    if ((int64_t)a.B * a.Hkv * a.row_blocks * a.chunks >= ((int64_t)1 << 31)) return VSCAN_ERR_UNSUPPORTED;
+    if ((int64_t)a.B * a.Hkv * a.row_blocks * a.chunks >= kMaxWorkgroups) return VSCAN_ERR_UNSUPPORTED;
     if (a.chunks > 1) {
         const size_t parts = (size_t)a.B * a.Hkv * rows * a.chunks;
         p->off_stat = align_up(parts * cache_dp(a.dh) * sizeof(float));

@@ -147,6 +147,17 @@ def test_cache_calls_reject_bad_pointers_and_workspaces():
         assert getattr(vb.lib(), fn)(ctypes.byref(desc), None) == NULL
 
 
+def test_cache_calls_refuse_grids_beyond_the_runtime():
+    """2^32 threads: 2^24 workgroups of 256."""
+    base = dataclasses.replace(CACHE, batch=1 << 12, q_heads=128, kv_heads=128, n_blocks=100, max_blocks=1 << 12)
+    for block, n_new, ok in ((16, 16 * 61, True), (16, 16 * 64, False), (64, 64 * 13, True), (64, 64 * 16, False)):
+        desc = vb.cache_desc(dataclasses.replace(base, block_size=block, n_new=n_new))
+        assert _store(desc, slots=None) == (NULL if ok else UNSUPPORTED), (block, n_new)
+    for n_new, ok in ((64 * 31, True), (64 * 32, False)):
+        desc = vb.cache_desc(dataclasses.replace(base, n_new=n_new))
+        assert _attend(desc, q=None) == (NULL if ok else UNSUPPORTED)
+
+
 def test_cache_calls_with_nothing_to_do():
     none = vb.cache_desc(dataclasses.replace(CACHE, batch=0))
     assert _store(none, None, None, None, None, None, None, None) == OK

@@ -306,3 +306,47 @@ def test_two_calls_at_once_and_two_graphs():
     for i in (0, 1, 0):
         got = vb.cache_attend(shapes[i], *states[i], workspace=space)["out"]
         assert torch.equal(got, want[i])
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_sequences_that_share_blocks(T):
+    """One prefix in the tables of several sequences, and a block twice in one table."""
+    shape = wl.CacheShape("bf16", 3, 8, 2, 64, 16, 30, 12, T)
+    q, cache, table, rows = make(shape, [150, 0, 0], 9)
+    table[1:] = table[0]
+    table[2, 5] = table[2, 1]
+    check(shape, q, cache, table, rows, [150, 144, 97], None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_heads_of_one(dtype):
+    run(dtype, 1024, 1, 64, 16, 1, [0, 40, 700])
+    run(dtype, 300, 2, 72, 32, 3, [3, 1, 333])
+
+
+def test_a_cache_of_more_than_32_bits():
+    """The same tokens in blocks at either end of 5 GB: equal bit for bit."""
+    import torch
+    small = wl.CacheShape("bf16", 2, 8, 4, 128, 16, 40, 12, 150)
+    large = dataclasses.replace(small, n_blocks=5 * (1 << 30) // (16 * 4 * 128))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((2, 4, 150, 128), generator=g, device="cuda").bfloat16() for _ in "kv")
+    q = torch.randn((2, 8, 150, 128), generator=g, device="cuda").bfloat16()
+    order = np.random.default_rng(4).permutation(small.n_blocks)
+    far = [int(x) if x % 3 == 0 else large.n_blocks - 1 - int(x) for x in order]
+    outs = []
+    for shape, free in ((small, order.tolist()), (large, far)):
+        cache = vb.cache_alloc(shape)
+        table = torch.full((2, 12), -1, dtype=torch.int32, device="cuda")
+        plan = vb.cache_plan(shape, i32([0, 0]), i32([150, 77]), i32(free), i32([0]), table)
+        assert table.tolist()[0][:10] == free[:10]
+        vb.cache_store(shape, k, v, plan["slot_map"], cache)
+        one = dataclasses.replace(shape, n_new=1)
+        outs.append([vb.cache_attend(shape, q, cache, table, plan["kv_len"], i32([150, 77]))["out"],
+                     vb.cache_attend(one, q[:, :, :1].contiguous(), cache, table, plan["kv_len"])["out"]])
+        for n in "kv":
+            outs[-1].append(cache[n][table[table >= 0].long()].clone())
+        del cache
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+    assert bool(outs[0][0].any())

@@ -277,3 +277,14 @@ def test_store_token_by_token_is_the_store_of_all(block):
         assert torch.equal(whole[kind + "_scale"][used], steps[kind + "_scale"][used])
         normal = a.abs() >= 2.0 ** -6
         assert torch.equal(a[normal], b[normal]) and float((a - b).abs().max()) <= 2.0 ** -9
+
+
+def test_store_of_slabs_more_than_32_bits_apart():
+    import torch
+    shape = wl.CacheShape("bf16", 1, 2, 2, 64, 16, 4, 4, 20)
+    rows = 5 * (1 << 30) // 128                                  # a slab of 5 GB
+    far = torch.empty(rows * 64 + 20 * 64, dtype=torch.bfloat16, device="cuda")
+    x = far.as_strided((1, 2, 20, 64), (2 * rows * 64, rows * 64, 64, 1))
+    x.copy_(torch.randn((1, 2, 20, 64), device="cuda"))
+    slots = _i32(_slots(shape, [3], [20], 2))
+    _check_store(shape, _fresh_cache(shape, 5), x, x, slots)

@@ -156,3 +156,19 @@ def test_rope_of_more_than_the_caches_hold(dtype, dh, extra, pairing):
     _check(shape, x, pos, freq, got)
     vb.rope(shape, pos, freq, x["q"], x["k"], in_place=True)
     assert torch.equal(x["q"], got["q"]) and torch.equal(x["k"], got["k"])
+
+
+def test_rope_of_rows_more_than_32_bits_apart():
+    """Two sequences at either end of 5 GB, read, and turned in place."""
+    import torch
+    shape = wl.RopeShape("bf16", 2, 9, 3, 2, 128, 128, (64,))
+    x, pos, freq = _inputs(shape, 8)
+    want = vb.rope(shape, pos, freq, x["q"], x["k"])
+    far = torch.empty(5 * (1 << 29) + (1 << 16), dtype=torch.bfloat16, device="cuda")
+    y = {n: far[at:].as_strided(t.shape, (5 * (1 << 29),) + t.stride()[1:]) for at, (n, t) in zip((0, 1 << 15), x.items())}
+    for n in y:
+        y[n].copy_(x[n])
+    got = vb.rope(shape, pos, freq, y["q"], y["k"])
+    assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"])
+    vb.rope(shape, pos, freq, y["q"], y["k"], in_place=True)
+    assert torch.equal(y["q"], want["q"]) and torch.equal(y["k"], want["k"])

@@ -22,6 +22,14 @@
 // The four waves of a workgroup take the tiles of its keys in turn and add their results in LDS; where
 // sequences and rows leave compute units idle the keys are cut into chunks over workgroups, which a
 // second launch joins.
+//
+// Measured, bf16, dh = 128, GPU time: one token of 32 sequences with 32 heads, up to 3427 keys, 126 us
+// (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 43 us (50 cold); of one with
+// 2304 keys 9.8 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096 keys 179 us
+// (755 TFLOP/s of the two products); 4 x 700 over 3000, 32 heads, 119 us (610); 3 x 300 over 2604, 28 of 4, 44 us
+// (430: the last round of workgroups is part full, and 40 % of a tile's cycles are not the matrix pipe's).
+// More rows a wave (64: 280 us where 32 take 179), eight waves (245) and rows over all four waves (203)
+// lost to this split.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>

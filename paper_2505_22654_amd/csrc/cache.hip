@@ -112,7 +112,10 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(PlanArgs a,
 // and keeps them while the largest absolute value of the page's new rows gives the scale.  After
 // rounding it holds 32 bytes that belong to pieces of its neighbours: one exchange (k) or a 4x4
 // transposition (v) between lanes of a quad leaves two whole 16-byte pieces of the page per unit.
-// Bound: HBM (2 or 4 bytes in and one out per value).
+// Bound: HBM (2 or 4 bytes in and one out per value).  32 sequences of up to 1267 tokens, 32 heads x 128 in
+// bf16 (803 MB): 155 us where the caches hold a part, 190 us cold (4.2 TB/s; a copy 5.0); one token of each
+// 4.6 us, a launch's latency.  Cold, with the pages of 4 heads side by side 184 us, of all heads 187; plain
+// loads 188; stores with the non-temporal hint 258, as no store fills a line by itself.
 constexpr int kStoreThreads = 256;
 
 // least e with amax <= 448 * 2^e (448 = 1.75 * 2^8), held inside what a scale may be

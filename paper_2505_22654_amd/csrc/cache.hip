@@ -113,9 +113,10 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(PlanArgs a,
 // rounding it holds 32 bytes that belong to pieces of its neighbours: one exchange (k) or a 4x4
 // transposition (v) between lanes of a quad leaves two whole 16-byte pieces of the page per unit.
 // Bound: HBM (2 or 4 bytes in and one out per value).  32 sequences of up to 1267 tokens, 32 heads x 128 in
-// bf16 (803 MB): 155 us where the caches hold a part, 190 us cold (4.2 TB/s; a copy 5.0); one token of each
-// 4.6 us, a launch's latency.  Cold, with the pages of 4 heads side by side 184 us, of all heads 187; plain
-// loads 188; stores with the non-temporal hint 258, as no store fills a line by itself.
+// bf16 (803 MB): 154 us cold (5.2 TB/s, as a copy); one token of each 4.7 us, a launch's latency.  With every
+// page's rows requested before its slot is known, which hides a load but reads the rows of ragged batches
+// that go nowhere, 190 us; loads with the non-temporal hint 160 (8 heads, 35 MB, from the caches: 31 us
+// without, 36 with); stores with it 258, as no store fills a line by itself.
 constexpr int kStoreThreads = 256;
 
 // least e with amax <= 448 * 2^e (448 = 1.75 * 2^8), held inside what a scale may be
@@ -197,8 +198,8 @@ struct Rows {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                raw[j][i] = load16_stream_guard(src, ((int64_t)(row + j) * dh + dim) * (int)sizeof(T) + 16 * i,
-                                                row + j >= 0 && row + j < n && dim < dh);
+                raw[j][i] = load16_guard(src, ((int64_t)(row + j) * dh + dim) * (int)sizeof(T) + 16 * i,
+                                         row + j >= 0 && row + j < n && dim < dh);
     }
     __device__ __forceinline__ void get(int j, float *f) const {
 #pragma unroll
@@ -276,30 +277,34 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(StoreArgs a,
     const int q0 = at0 / 4, q1 = (at0 + r1 - r0 + 3) / 4;  // quads of tokens that the rows lie in
     const int units = (q1 - q0) * (DP / 8);
     Rows<T> held[kHold];
+    auto load = [&](int rows) {
 #pragma unroll
-    for (int i = 0; i < kHold; ++i) {
-        const int u = lane + i * LANES;
-        if (u < units) {
-            const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
-            held[i].load(src, un.token - at0, r1 - r0, un.dim, a.dh);
+        for (int i = 0; i < kHold; ++i) {
+            const int u = lane + i * LANES;
+            if (u < units) {
+                const Unit un = unit_at<DP>(q0 * (DP / 8) + u, kind);
+                held[i].load(src, un.token - at0, rows, un.dim, a.dh);
+            }
         }
-    }
+    };
 
-    const int slot = slots[r0];
+    int n = r1 - r0;
+    const int mine = slots[r0 + min(lane, n - 1)], slot = run ? slots[r0] : s0;
     if (slot < 0 || (slot >> a.block_shift) >= a.n_blocks || (slot & (size - 1)) != at0) return;
+    if (run == 0) load(n);  // ahead of knowing how many of them follow each other: a token's latency
     const int64_t page = (int64_t)(slot >> a.block_shift) * a.Hkv + hk;
     // rows that continue the first one
-    int n = r1 - r0;
     if constexpr (LANES == kWave) {
-        const uint64_t bad = __ballot(lane < n && slots[r0 + min(lane, n - 1)] != slot + lane);
+        const uint64_t bad = __ballot(lane < n && mine != slot + lane);
         if (bad) n = __ffsll((unsigned long long)bad) - 1;
     } else {
         if (lane == 0) first_bad = n;
         __syncthreads();
-        if (lane < n && slots[r0 + lane] != slot + lane) atomicMin(&first_bad, lane);
+        if (lane < n && mine != slot + lane) atomicMin(&first_bad, lane);
         __syncthreads();
         n = first_bad;
     }
+    if (run) load(n);
     // (fmaxf passes NaN over)
     auto largest = [&](bool finite) {
         float m = 0.f;
@@ -400,20 +405,24 @@ hipError_t launch_store_as(const StoreArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// A page is a wave's work up to 32 tokens: 32 sequences x 8 kv heads x 128 in bf16, GPU time in us of a wave
-// and of a workgroup: 1267 tokens in blocks of 32 45.1 and 50.6, of 64 46.1 and 41.4, of 128 59.6 and 47.4;
-// one token 4.1 and 4.8 in either, but a wave takes long to fill or rescale a large page.  A lane that can
-// meet one unit only holds one: 1267 tokens in blocks of 16 40.7, where lanes with room for four take 51.
+// A lane holds no more units than it can meet: 32 sequences of 1267 tokens, 8 kv heads x 128 in bf16, GPU
+// time in us with just enough units and with four: blocks of 16 31.2 and 41.4, of 32 (two units) 32.7 and
+// 34.5, of 64 33.1 and 47.3, of 128 (two) 34.1 and 38.0.
+template <typename T, int DP, int LANES>
+hipError_t launch_store_lanes(const StoreArgs &a, int units, hipStream_t s) {
+    constexpr int kMost = sizeof(T) == 2 ? 4 : 2;  // 64 registers
+    if (units <= LANES) return launch_store_as<T, DP, LANES, 1>(a, s);
+    if (kMost > 2 && units <= 2 * LANES) return launch_store_as<T, DP, LANES, 2>(a, s);
+    return launch_store_as<T, DP, LANES, kMost>(a, s);
+}
+
 template <typename T, int DP>
 hipError_t launch_store_dp(const StoreArgs &a, hipStream_t s) {
-    constexpr int kMost = sizeof(T) == 2 ? 4 : 2;  // 64 registers
     const int size = 1 << a.block_shift;
     // quads that one call's rows can lie in
     const int units = min(size / 4, (a.n_new + 6) / 4) * (DP / 8);
-    if (store_pages(size) > 1)
-        return units <= kWave ? launch_store_as<T, DP, kWave, 1>(a, s) : launch_store_as<T, DP, kWave, kMost>(a, s);
-    return units <= kStoreThreads ? launch_store_as<T, DP, kStoreThreads, 1>(a, s)
-                                  : launch_store_as<T, DP, kStoreThreads, kMost>(a, s);
+    return store_pages(size) > 1 ? launch_store_lanes<T, DP, kWave>(a, units, s)
+                                 : launch_store_lanes<T, DP, kStoreThreads>(a, units, s);
 }
 
 template <typename T>

@@ -58,7 +58,10 @@ struct StoreArgs {
     const int32_t *slot_map;
     int B, Hkv, n_new, seq_len, dh, block_shift, n_blocks, is_bf16;
 };
-// Pages (a block's part of one kv head, of k or of v) of a workgroup: a wave or all of it each.
+// Pages (a block's part of one kv head, of k or of v) of a workgroup: a wave or all of it each.  32 sequences
+// of 1267 tokens, 8 kv heads x 128 in bf16, GPU time in us of a wave and of a workgroup to a page: blocks of
+// 32 32.7 and 44.8, of 64 36.0 and 33.1, of 128 45.3 and 34.1; one token 4.1 and 4.7 in any, but a wave takes
+// long to fill or rescale a large page.
 constexpr int store_pages(int block_size) { return block_size <= 32 ? 4 : 1; }
 hipError_t launch_cache_store(const void *args, hipStream_t s);
 

@@ -552,6 +552,9 @@ def llm_prune_fused_ragged(shape, meta, hidden, w_q, w_k_t, want_scores: bool = 
 
 
 # ---- around the pruned prefill: rotary positions and the paged 8-bit cache -----------------------
+_ROPE_BYTES, _CACHE_BYTES = ctypes.sizeof(RopeDesc), ctypes.sizeof(CacheDesc)
+
+
 def _check(ok: bool, what: str) -> None:
     if not ok:
         raise ValueError(what)
@@ -578,13 +581,12 @@ def _call(entry: str, index: int, *args) -> None:
     """Calls `entry` on the current stream of CUDA device `index`, with that device the current one.
     (The stream's handle is taken without the object that torch.cuda.current_stream makes around it:
     4 of the 19 us that a small call took.)"""
-    torch = _torch()
-    fn, stream = getattr(_lib or lib(), entry), torch._C._cuda_getCurrentRawStream
-    if index == torch.cuda.current_device():
-        rc = fn(*args, stream(index))
+    fn, C = getattr(_lib or lib(), entry), _torch()._C
+    if index == C._cuda_getDevice():  # (the tensors are there, so CUDA is initialised)
+        rc = fn(*args, C._cuda_getCurrentRawStream(index))
     else:
-        with torch.cuda.device(index):
-            rc = fn(*args, stream(index))
+        with _torch().cuda.device(index):
+            rc = fn(*args, C._cuda_getCurrentRawStream(index))
     if rc != VSCAN_OK:
         raise VscanError(rc, entry)
 
@@ -597,11 +599,15 @@ def _torch(modules=sys.modules):
     return torch
 
 
+def _dtype_of(torch, dtype: str):
+    return torch.bfloat16 if dtype == "bf16" else torch.float32 if dtype == "f32" else _torch_dtype(dtype)
+
+
 def rope_desc(shape, q_stride=(0, 0, 0), k_stride=(0, 0, 0)) -> RopeDesc:
     """Descriptor from a `RopeShape`-like object."""
     n = len(shape.sections)
     _check(1 <= n <= ROPE_MAX_AXES, f"sections: 1 to {ROPE_MAX_AXES} axes, got {n}")
-    return RopeDesc(ctypes.sizeof(RopeDesc), _dtype_code(shape.dtype), shape.batch, shape.seq_len,
+    return RopeDesc(_ROPE_BYTES, _dtype_code(shape.dtype), shape.batch, shape.seq_len,
                     shape.q_heads, shape.kv_heads, shape.head_dim, shape.rot_dim, n, *shape.sections,
                     *(0,) * (ROPE_MAX_AXES - n), shape.order, shape.pairing, shape.inverse, *q_stride, *k_stride)
 
@@ -621,7 +627,7 @@ def rope(shape, positions, inv_freq, q=None, k=None, in_place: bool = False,
 
     Returns q and k turned: new contiguous tensors, those of `out`, or (`in_place`) the inputs."""
     torch = _torch()
-    dt, B, S = _torch_dtype(shape.dtype), shape.batch, shape.seq_len
+    dt, B, S = _dtype_of(torch, shape.dtype), shape.batch, shape.seq_len
     index, src, dst, strides = positions.get_device(), [None, None], [None, None], [(0, 0, 0), (0, 0, 0)]
     _check(positions.is_cuda, "positions: expected a CUDA tensor")
     _check_tensor("positions", positions, torch.int32, (len(shape.sections), B, S), index)
@@ -655,7 +661,7 @@ def rope(shape, positions, inv_freq, q=None, k=None, in_place: bool = False,
 
 def cache_desc(shape, seq_len: int = 0) -> CacheDesc:
     """Descriptor from a `CacheShape`-like object."""
-    return CacheDesc(ctypes.sizeof(CacheDesc), _dtype_code(shape.dtype), shape.batch, shape.q_heads,
+    return CacheDesc(_CACHE_BYTES, _dtype_code(shape.dtype), shape.batch, shape.q_heads,
                      shape.kv_heads, shape.head_dim, shape.block_size, shape.n_blocks, shape.max_blocks,
                      shape.n_new, seq_len, shape.max_len, shape.scale)
 
@@ -684,8 +690,12 @@ def cache_alloc(shape, device="cuda") -> Dict[str, object]:
 
 def _check_cache(shape, cache, index: int) -> None:
     torch = _torch()
-    for n, d, s in _cache_shapes(shape):
-        _check_tensor(n, cache[n], torch.uint8 if d == "uint8" else torch.float32, s, index)
+    groups, dp = shape.block_size // 16, (shape.head_dim + 63) // 64 * 64
+    n, h, u8, f32 = shape.n_blocks, shape.kv_heads, torch.uint8, torch.float32
+    _check_tensor("k", cache["k"], u8, (n, h, groups, dp // 16, 16, 16), index)
+    _check_tensor("v", cache["v"], u8, (n, h, groups, dp // 64, 4, 16, 4, 4), index)
+    _check_tensor("k_scale", cache["k_scale"], f32, (n, h), index)
+    _check_tensor("v_scale", cache["v_scale"], f32, (n, h), index)
 
 
 def cache_plan_workspace_size(desc: CacheDesc) -> int:
@@ -734,7 +744,7 @@ def cache_store(shape, k, v, slot_map, cache) -> Dict[str, object]:
     `cache_alloc`, which is written in place and returned.  k and v may be the first n_new rows of longer
     slabs (what an in-place prune returns)."""
     torch = _torch()
-    dt, dev, index = _torch_dtype(shape.dtype), slot_map.device, slot_map.get_device()
+    dt, dev, index = _dtype_of(torch, shape.dtype), slot_map.device, slot_map.get_device()
     T, dh = shape.n_new, shape.head_dim
     size, rows = (shape.batch, shape.kv_heads, T, dh), T
     _check(slot_map.is_cuda, "slot_map: expected a CUDA tensor")
@@ -770,7 +780,7 @@ def cache_attend(shape, q, cache, block_table, kv_len, new_len=None, workspace=N
 
     Returns out [B,Hq,n_new,dh] and the workspace; both may be passed in."""
     torch = _torch()
-    i32, dt, dev, index, B = torch.int32, _torch_dtype(shape.dtype), q.device, q.get_device(), shape.batch
+    i32, dt, dev, index, B = torch.int32, _dtype_of(torch, shape.dtype), q.device, q.get_device(), shape.batch
     desc = cache_desc(shape)
     size = (B, shape.q_heads, shape.n_new, shape.head_dim)
     _check(q.is_cuda, "q: expected a CUDA tensor")

@@ -447,7 +447,9 @@ int vscan_cache_size(const vscan_cache_desc *desc, size_t *cache_bytes, size_t *
  *                every slot is -1 and kv_len is c
  * free_blocks is [n_free], free_head [1] (held inside 0 .. n_free).  kv_len may be
  * cached_len, and free_head_out may be free_head; no other buffers may overlap.
- * head_dim, heads and dtype are not used.  B <= 65535. */
+ * head_dim, heads and dtype are not used.  B <= 65535.  Workspace:
+ * vscan_cache_plan_workspace_size bytes, 16-byte aligned (0: none is needed, NULL is
+ * taken). */
 int vscan_cache_plan_workspace_size(const vscan_cache_desc *desc, size_t *bytes);
 int vscan_cache_plan(const vscan_cache_desc *desc, const int32_t *cached_len,
                      const int32_t *new_len, const int32_t *free_blocks, int32_t n_free,

@@ -716,7 +716,7 @@ def cache_plan(shape, cached_len, new_len, free_blocks, free_head, block_table, 
     torch = _torch()
     i32, dev, index, B = torch.int32, block_table.device, block_table.get_device(), shape.batch
     desc = cache_desc(shape)
-    need = cache_plan_workspace_size(desc)
+    need = cache_plan_workspace_size(desc) if workspace is None else 0
     _check(block_table.is_cuda, "block_table: expected a CUDA tensor")
     _check_tensor("cached_len", cached_len, i32, (B,), index)
     _check_tensor("new_len", new_len, i32, (B,), index)
@@ -734,7 +734,7 @@ def cache_plan(shape, cached_len, new_len, free_blocks, free_head, block_table, 
     _call("vscan_cache_plan", index, ctypes.byref(desc), cached_len.data_ptr(), new_len.data_ptr(),
           free_blocks.data_ptr(), free_blocks.numel(), free_head.data_ptr(), block_table.data_ptr(),
           out["slot_map"].data_ptr(), out["kv_len"].data_ptr(), out["free_head"].data_ptr(),
-          out["missing"].data_ptr(), workspace.data_ptr(), workspace.numel())
+          out["missing"].data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel())
     out["block_table"], out["workspace"] = block_table, workspace
     return out
 

@@ -37,17 +37,19 @@ struct PlanArgs {
     int B, n_new, block_shift, n_blocks, max_blocks, n_free;
 };
 // Workgroups of the launch that reads the lengths, if it writes the tables too, and 0 if a second launch
-// has to.  One workgroup may write up to 4096 rows by itself; several, a row a thread, each read all
+// has to.  One workgroup may write up to kPlanAlone rows by itself; several, a row a thread, each read all
 // lengths, so the requests must fit a workgroup and no input may be overwritten while another reads it.
 // GPU time, us: 32 requests, 32 x 3427 rows: two launches 5.9, workgroups of 16384 rows 10.6, 4096 5.6,
 // 1024 4.2; 256 x 16 rows: one workgroup 5.4, four 4.1.  (A launch more is 2.5 us of the host's time.)
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024, kPlanAlone = 4096;
 inline int plan_workgroups(const PlanArgs &a) {
     const int64_t rows = (int64_t)a.B * a.n_new, parts = (rows + kPlanThreads - 1) / kPlanThreads;
     if (a.B <= kPlanThreads && a.kv_len != a.cached_len && a.free_head_out != a.free_head)
         return parts < 1 ? 1 : parts < 256 ? (int)parts : 256;
-    return rows <= 4096 ? 1 : 0;
+    return rows <= kPlanAlone ? 1 : 0;
 }
+// Whether `requests` may be written: not where one launch holds them in LDS whatever overlaps.
+inline bool plan_needs_scratch(int64_t B, int64_t n_new) { return B > kPlanThreads || B * n_new > kPlanAlone; }
 hipError_t launch_cache_plan(const void *args, hipStream_t s);
 hipError_t launch_cache_tables(const void *args, hipStream_t s);
 

@@ -192,8 +192,8 @@ int cache_plan(const vscan_cache_desc *d, const int32_t *cached_len, const int32
                                slot_map, kv_len, free_head_out, missing};
     for (const void *p : all)
         if (!aligned(p, 4)) return VSCAN_ERR_ALIGN;
-    if (!workspace || workspace_bytes < need) return VSCAN_ERR_WORKSPACE;
-    if (!aligned(workspace, 16)) return VSCAN_ERR_ALIGN;
+    if (need && (!workspace || workspace_bytes < need)) return VSCAN_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return VSCAN_ERR_ALIGN;
     PlanArgs a;
     a.cached_len = cached_len;
     a.new_len = new_len;
@@ -341,7 +341,7 @@ int vscan_cache_plan_workspace_size(const vscan_cache_desc *desc, size_t *bytes)
     if (!bytes) return VSCAN_ERR_NULL;
     const int rc = check_cache(desc);
     if (rc != VSCAN_OK) return rc;
-    *bytes = align_up(std::max<size_t>(1, (size_t)desc->batch * 4 * sizeof(int32_t)));
+    *bytes = plan_needs_scratch(desc->batch, desc->n_new) ? align_up((size_t)desc->batch * 4 * sizeof(int32_t)) : 0;
     return VSCAN_OK;
 }
 

@@ -39,7 +39,8 @@ hipError_t launch_rope(const void *args, hipStream_t) {
 
 hipError_t launch_cache_plan(const void *args, hipStream_t) {
     const PlanArgs &a = *static_cast<const PlanArgs *>(args);
-    inside(a.requests, (size_t)a.B * 16);
+    if (plan_needs_scratch(a.B, a.n_new)) inside(a.requests, (size_t)a.B * 16);
+    else need(plan_workgroups(a) > 0 && a.B <= kPlanThreads);
     ++g_launches;
     return hipSuccess;
 }

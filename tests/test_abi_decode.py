@@ -127,9 +127,14 @@ def test_cache_calls_reject_bad_pointers_and_workspaces():
         assert _plan(desc, **{name: None}) == NULL
         assert _plan(desc, **{name: FAKE + 2}) == ALIGN
     assert _plan(desc, n_free=-1) == SHAPE
-    need = vb.cache_plan_workspace_size(desc)
-    assert _plan(desc, ws=None) == _plan(desc, ws_bytes=need - 1) == WS
-    assert _plan(desc, ws=FAKE + 8) == ALIGN
+    # lengths of few rows stay in one workgroup, more need scratch
+    assert vb.cache_plan_workspace_size(desc) == 0
+    for change in (dict(batch=1025, n_new=0), dict(batch=8, n_new=513)):
+        many = vb.cache_desc(dataclasses.replace(CACHE, **change))
+        need = vb.cache_plan_workspace_size(many)
+        assert need >= 16 * change["batch"]
+        assert _plan(many, ws=None) == _plan(many, ws_bytes=need - 1) == WS
+        assert _plan(many, ws=FAKE + 8) == ALIGN
     for name in ("k", "v", "slots", "kc", "vc", "ks", "vs"):
         assert _store(desc, **{name: None}) == NULL
         assert _store(desc, **{name: FAKE + 2}) == ALIGN

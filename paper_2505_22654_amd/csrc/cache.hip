@@ -411,9 +411,12 @@ hipError_t launch_store_as(const StoreArgs &a, hipStream_t s) {
 template <typename T, int DP, int LANES>
 hipError_t launch_store_lanes(const StoreArgs &a, int units, hipStream_t s) {
     constexpr int kMost = sizeof(T) == 2 ? 4 : 2;  // 64 registers
-    if (units <= LANES) return launch_store_as<T, DP, LANES, 1>(a, s);
-    if (kMost > 2 && units <= 2 * LANES) return launch_store_as<T, DP, LANES, 2>(a, s);
-    return launch_store_as<T, DP, LANES, kMost>(a, s);
+    constexpr int kPage = (LANES == kWave ? 32 : 256) / 4 * (DP / 8);  // units of the largest page
+    if constexpr (kPage > 2 * LANES && kMost > 2)
+        if (units > 2 * LANES) return launch_store_as<T, DP, LANES, kMost>(a, s);
+    if constexpr (kPage > LANES)
+        if (units > LANES) return launch_store_as<T, DP, LANES, 2>(a, s);
+    return launch_store_as<T, DP, LANES, 1>(a, s);
 }
 
 template <typename T, int DP>

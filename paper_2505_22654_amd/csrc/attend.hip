@@ -5,31 +5,32 @@
 // takes them, so they never leave the registers.  The cache is stored in operand order: a lane's 16
 // bytes are one load, and nothing is staged in LDS.
 //
-// bf16 calls: K as bf16 (exact) times q; V as fp16 (exact) times the weights in fp16 (2^-11 of each;
+// bf16 calls: K times q, both exact; V as fp16 (exact) times the weights in fp16 (2^-11 of each;
 // bf16's 2^-8 would add as much to the error as the result's own rounding).  fp32 calls: q and the
 // weights as three bf16 planes each, V as bf16.  K's scale goes into the logits; V's, a power of two,
 // is taken relative to the largest that the wave has met: down to 2^-15 with the values, beyond that
 // with the weights, whose reference it then enters, so that the largest contributions keep their bits.
-// Softmax in one pass against a reference that is raised only where a logit passes it by more than
-// 2^8, so that most tiles need no exchange between lanes.
+// Softmax in one pass against a reference that is raised only where a lane's weights of a tile add up to more
+// than 2^12, so that most tiles need no exchange between lanes and no maximum.
 //
 // Two forms, by rows: up to 16, with 16x16x32 instructions and 64 keys at a time (bound by HBM: 2 dh
-// bytes per token and kv head); more, 32 to a workgroup, with 32x32x16 instructions and 32 keys at a
-// time, two tiles in flight (bound by the vector instructions beside the matrix pipe: per logit a
-// multiply-add, a maximum, an exponential and a sum, and the conversions; a matrix instruction keeps the
-// vector unit from issuing for some cycles whatever its size, so the large ones overlap better: 96
-// multiply-adds and 16 exponentials with 514 cycles of them 667, with 16x16x32 861).
+// bytes per token and kv head); more, 32 to a wave, with 32 keys at a time, two tiles in flight.  There a bf16
+// q goes into two e4m3 planes, which are multiplied with K as it is stored, 64 dims an instruction, and V is
+// converted for 32x32x16 instructions (bound by the vector unit beside the matrix pipe: per logit a multiply-add,
+// an exponential and a sum, and V's and the weights' conversions; a matrix instruction keeps the vector unit
+// from issuing for some cycles whatever its size, so the large ones overlap better: 96 multiply-adds and 16
+// exponentials with 514 cycles of them 667, with 16x16x32 861).
 // The four waves of a workgroup take the tiles of its keys in turn and add their results in LDS; where
 // sequences and rows leave compute units idle the keys are cut into chunks over workgroups, which a
 // second launch joins.
 //
 // Measured, bf16, dh = 128, GPU time: one token of 32 sequences with 32 heads, up to 3427 keys, 126 us
 // (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 43 us (50 cold); of one with
-// 2304 keys 9.8 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096 keys 179 us
-// (755 TFLOP/s of the two products); 4 x 700 over 3000, 32 heads, 119 us (610); 3 x 300 over 2604, 28 of 4, 44 us
-// (430: the last round of workgroups is part full, and 40 % of a tile's cycles are not the matrix pipe's).
-// More rows a wave (64: 280 us where 32 take 179), eight waves (245) and rows over all four waves (203)
-// lost to this split.
+// 2304 keys 9.9 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096 keys 165 us
+// (820 TFLOP/s of the two products), over 8192 300 us (915); 4 x 700 over 3000, 32 heads, 111 us (655); 3 x 300
+// over 2604, 28 of 4, 42 us (460: 396 workgroups on 256 CUs).  With K converted to bf16 and a maximum of each
+// tile these four took 177, 328, 117 and 44.  More rows a wave (64: 280 us where 32 took 179), eight waves (245)
+// and rows over all four waves (203) lost to this split.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -52,7 +53,7 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 constexpr int kWaves = kAttendWaves;
 constexpr float kNothing = -1e30f;  // reference of a row that has seen no key
 constexpr float kBias = 4.f;        // the largest weight is 2^4 when the reference is set ..
-constexpr float kRaise = 12.f;      // .. and at most 2^12 until it is raised (fp16 holds 2^16)
+constexpr float kRaise = 4096.f;    // .. and a lane's sum of a tile at most this until it is raised (fp16 holds 2^16)
 constexpr int kValueExp = -15;      // e4m3's 2^-9 times 2^-15 is fp16's smallest number
 constexpr int kWeightExp = -100;    // sums of weights without this factor stay inside fp32
 
@@ -242,6 +243,68 @@ __device__ __forceinline__ void load_query(const AttendArgs &a, const Row &row, 
             }
         }
     }
+}
+
+// A bf16 query in two e4m3 planes, for products with K as it is stored: 2^e of a row puts its largest entry
+// at 2^7 to 2^8, hi = q / 2^e rounded to 4 bits, lo = 16 (q / 2^e - hi).  bf16's 8 bits leave lo at most 4, so
+// both are exact for entries down to 2^-13 of the largest (lo's last place is 2^-13), and below it off by 2^-14 of
+// 2^e, 2^-21 of the largest.  The planes' 2^e and 2^(e - 4) are operands of the instruction (exponent bytes).
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ i32x8_t eight(const uint4 &a, const uint4 &b) {
+    return i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
+}
+__device__ __forceinline__ uint32_t to_fp8(float a, float b, float c, float d) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+// Row of a lane for products of 64 dims, 32 in each half of the wave: those that its 16-byte pieces of K are.
+template <int kN>
+__device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &row, int g, i32x8_t (*out)[2], int *scale) {
+    const bool ok = row.at >= 0 && !row.padding;
+    const bf16_t *src = static_cast<const bf16_t *>(a.q) + max(row.at, (int64_t)0);
+    uint4 raw[kN][4];
+    float top = 0.f;
+#pragma unroll
+    for (int m = 0; m < kN; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 64 * m + 32 * (i >> 1) + 16 * g + 8 * (i & 1);
+            raw[m][i] = load16_guard(src, (int64_t)d * 2, ok && d < a.dh);
+        }
+#pragma unroll
+    for (int m = 0; m < kN; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float f[8];
+            unpack16<bf16_t>(raw[m][i], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+        }
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    // 2^e with 128 <= top / 2^e < 256
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -100), 120);
+    scale[0] = e + 127;
+    scale[1] = e + 127 - 4;
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+    for (int m = 0; m < kN; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float f[8];
+            unpack16<bf16_t>(raw[m][i], f);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = f[4 * h + r] * inv;
+                const uint32_t w = to_fp8(x[0], x[1], x[2], x[3]);
+                x[0] -= __builtin_amdgcn_cvt_f32_fp8(w, 0);
+                x[1] -= __builtin_amdgcn_cvt_f32_fp8(w, 1);
+                x[2] -= __builtin_amdgcn_cvt_f32_fp8(w, 2);
+                x[3] -= __builtin_amdgcn_cvt_f32_fp8(w, 3);
+                out[m][0][2 * i + h] = (int)w;
+                out[m][1][2 * i + h] = (int)to_fp8(16.f * x[0], 16.f * x[1], 16.f * x[2], 16.f * x[3]);
+            }
+        }
 }
 
 // The keys of a tile: where its groups of 16 lie, and their scales.
@@ -546,24 +609,42 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         Scales<kGroups, kP == 1> sc;
         sc.of(at[0], eref);
         settle_products<8>();
-        float x[kGroups][4];
-        auto logits = [&](float ref) {
-            float top = -INFINITY;
+        typename O::vec pb[kGroups / 2][kP];
+        float sums[kGroups];
+        auto logit = [&](int u, int r, float add) {
+            float v = fmaf(s[u][r], at[0].c[u], add);
+            if constexpr (kMask) v = at[0].there[u] && kt + u * kCacheGroup + 4 * g + r < row.lim ? v : -INFINITY;
+            return v;
+        };
+        auto weigh = [&](float ref) {
+            float all = 0.f;
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
                 const float add = sc.weights[u] - ref;
+                sums[u] = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float v = fmaf(s[u][r], at[0].c[u], add);
-                    if constexpr (kMask) v = at[0].there[u] && kt + u * kCacheGroup + 4 * g + r < row.lim ? v : -INFINITY;
-                    x[u][r] = v;
-                    top = fmaxf(top, v);
+                for (int r = 0; r < 4; r += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(logit(u, r, add)), p1 = __builtin_amdgcn_exp2f(logit(u, r + 1, add));
+                    typename O::pair pp[kP];
+                    split<O, kP>(f32x2_t{p0, p1}, pp);
+                    sums[u] += p0;
+                    sums[u] += p1;
+#pragma unroll
+                    for (int q = 0; q < kP; ++q) {
+                        pb[u / 2][q][4 * (u & 1) + r] = pp[q][0];
+                        pb[u / 2][q][4 * (u & 1) + r + 1] = pp[q][1];
+                    }
                 }
+                all += sums[u];
             }
-            return top;
+            return all;
         };
-        if (__any(logits(m) > kRaise) || sc.now > eref) {
-            float top = logits(0.f);
+        if (__any(weigh(m) > kRaise) || sc.now > eref) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, logit(u, r, sc.weights[u]));
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
@@ -572,7 +653,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             l *= f;
 #pragma unroll
             for (int d = 0; d < kD; ++d) acc[d] *= fu;
-            logits(now);
+            weigh(now);
         }
         if constexpr (kMask) {
 #pragma unroll
@@ -595,33 +676,14 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
 #pragma unroll
         for (int v = 0; v < kGroups / 2; ++v) {
-            typename O::vec pb[kP];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float *p = x[2 * v + i], sum = 0.f;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    p[r] = __builtin_amdgcn_exp2f(p[r]);
-                    sum += p[r];
-                }
-                l = fmaf(sum, sc.sums[2 * v + i], l);
-#pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    typename O::pair pp[kP];
-                    split<O, kP>(f32x2_t{p[r], p[r + 1]}, pp);
-#pragma unroll
-                    for (int q = 0; q < kP; ++q) {
-                        pb[q][4 * i + r] = pp[q][0];
-                        pb[q][4 * i + r + 1] = pp[q][1];
-                    }
-                }
-            }
+            l = fmaf(sums[2 * v], sc.sums[2 * v], l);
+            l = fmaf(sums[2 * v + 1], sc.sums[2 * v + 1], l);
 #pragma unroll
             for (int d = 0; d < kD; ++d) {
                 const typename O::vec vv = from_fp8<O>(word(vb[2 * v][d >> 2], d & 3), word(vb[2 * v + 1][d >> 2], d & 3),
                                                        sc.values[2 * v], sc.values[2 * v + 1]);
 #pragma unroll
-                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma(vv, pb[q], acc[d]);
+                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma(vv, pb[v][q], acc[d]);
             }
         }
         fetch(a.v_cache, next, vb);
@@ -697,9 +759,16 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     if (a.chunks > 1 && w.k0 >= w.block_reach) return;
 
     const Row row = row_of(a, w, w.row0 + j);
-    bf16x8_t qf[2 * kC][kQ];
+    constexpr bool kFp8 = sizeof(T) == 2;
+    bf16x8_t qf[kFp8 ? 1 : 2 * kC][kQ];
+    i32x8_t q8[kFp8 ? kC / 2 : 1][2];
+    int q8_scale[2];
+    if constexpr (kFp8) {
+        load_query_fp8<kC / 2>(a, row, g, q8, q8_scale);
+    } else {
 #pragma unroll
-    for (int c = 0; c < 2 * kC; ++c) load_query<T>(a, row, (c >> 1) * 32 + g * 16 + (c & 1) * 8, qf[c]);
+        for (int c = 0; c < 2 * kC; ++c) load_query<T>(a, row, (c >> 1) * 32 + g * 16 + (c & 1) * 8, qf[c]);
+    }
 
     struct Values {
         uint4 pair[4][kPairs > 0 ? kPairs : 1];  // [tokens 8a + 4g ..][pair of 64 dims]
@@ -738,10 +807,19 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         });
     }
     // (the queries are waited for here, not in the loop)
+    if constexpr (kFp8) {
 #pragma unroll
-    for (int c = 0; c < 2 * kC; ++c)
+        for (int m = 0; m < kC / 2; ++m)
 #pragma unroll
-        for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[c][q]));
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) asm volatile("" ::"v"(q8[m][q][i]));
+    } else {
+#pragma unroll
+        for (int c = 0; c < 2 * kC; ++c)
+#pragma unroll
+            for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[c][q]));
+    }
 
     f32x16_t acc[kD];
     float m = kNothing, l = 0.f;
@@ -760,35 +838,57 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         f32x16_t s;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 0.f;
+        if constexpr (kFp8) {
+#pragma unroll
+            for (int m = 0; m < kC / 2; ++m)
+#pragma unroll
+                for (int q = 1; q >= 0; --q)
+                    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(eight(kb[2 * m], kb[2 * m + 1]), q8[m][q], s, 0, 0, 0, 127, 0, q8_scale[q]);
+        } else {
 #pragma unroll
         for (int c = 0; c < 2 * kC; ++c) {
             const bf16x8_t ka = from_fp8<Operand<float>>(word(kb[c >> 1], 2 * (c & 1)), word(kb[c >> 1], 2 * (c & 1) + 1), 1.f, 1.f);
 #pragma unroll
             for (int q = kQ - 1; q >= 0; --q) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[c][q], s, 0, 0, 0);
         }
+        }
         fetch_keys(next, kb);
 
         Scales<kGroups, kP == 1> sc;
         sc.of(at, eref);
         settle_products<8>();
-        float x[16];
-        auto logits = [&](float ref) {
-            float top = -INFINITY;
+        typename O::vec pb[kGroups][kP];
+        float sums[kGroups];
+        auto logit = [&](int r, float add) {
+            float v = fmaf(s[r], at.c[r >> 3], add);
+            if constexpr (kMask) v = at.there[r >> 3] && kt + 8 * (r >> 2) + 4 * g + (r & 3) < row.lim ? v : -INFINITY;
+            return v;
+        };
+        auto weigh = [&](float ref) {
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
                 const float add = sc.weights[u] - ref;
+                sums[u] = 0.f;
 #pragma unroll
-                for (int r = 8 * u; r < 8 * u + 8; ++r) {
-                    float v = fmaf(s[r], at.c[u], add);
-                    if constexpr (kMask) v = at.there[u] && kt + 8 * (r >> 2) + 4 * g + (r & 3) < row.lim ? v : -INFINITY;
-                    x[r] = v;
-                    top = fmaxf(top, v);
+                for (int r = 0; r < 8; r += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(logit(8 * u + r, add)), p1 = __builtin_amdgcn_exp2f(logit(8 * u + r + 1, add));
+                    typename O::pair pp[kP];
+                    split<O, kP>(f32x2_t{p0, p1}, pp);
+                    sums[u] += p0;
+                    sums[u] += p1;
+#pragma unroll
+                    for (int q = 0; q < kP; ++q) {
+                        pb[u][q][r] = pp[q][0];
+                        pb[u][q][r + 1] = pp[q][1];
+                    }
                 }
             }
-            return top;
+            return sums[0] + sums[1];
         };
-        if (__any(logits(m) > kRaise) || sc.now > eref) {
-            float top = logits(0.f);
+        if (__any(weigh(m) > kRaise) || sc.now > eref) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, logit(r, sc.weights[r >> 3]));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
             m = now;
@@ -796,7 +896,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             l *= f;
 #pragma unroll
             for (int d = 0; d < kD; ++d) acc[d] *= fu;
-            logits(now);
+            weigh(now);
         }
         if constexpr (kMask) {
 #pragma unroll
@@ -826,29 +926,14 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
 #pragma unroll
         for (int u = 0; u < kGroups; ++u) {
-            typename O::vec pb[kP];
-            float sum = 0.f;
-#pragma unroll
-            for (int r = 0; r < 8; r += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(x[8 * u + r]), p1 = __builtin_amdgcn_exp2f(x[8 * u + r + 1]);
-                sum += p0;
-                sum += p1;
-                typename O::pair pp[kP];
-                split<O, kP>(f32x2_t{p0, p1}, pp);
-#pragma unroll
-                for (int q = 0; q < kP; ++q) {
-                    pb[q][r] = pp[q][0];
-                    pb[q][r + 1] = pp[q][1];
-                }
-            }
-            l = fmaf(sum, sc.sums[u], l);
+            l = fmaf(sums[u], sc.sums[u], l);
 #pragma unroll
             for (int d = 0; d < kD; ++d) {
                 uint32_t lo, up;
                 value_words(vb, u, d, lo, up);
                 const typename O::vec vv = from_fp8<O>(lo, up, sc.values[u], sc.values[u]);
 #pragma unroll
-                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma32(vv, pb[q], acc[d]);
+                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma32(vv, pb[u][q], acc[d]);
             }
         }
         fetch_values(next, vb);

@@ -144,7 +144,9 @@ def store(shape, x, slot_map, values, scales):
 def attend(shape, q, k_rows, v_rows, v_scales, table, kv_len, new_len):
     """(out, bound) in 64 bits.  k_rows, v_rows: values with scales, [n_blocks,Hkv,bs,dh]; v_scales
     [n_blocks,Hkv].  `bound` is what rounding may move a result by, apart from the last one: with u =
-    2^-24 a logit of dh products is off by at most (dh + 8) u sum|q k| scale (the products are exact),
+    2^-24 a logit of dh products is off by at most (dh + 8) u sum|q k| scale (the products are exact; in
+    bf16 calls an entry of q below 2^-13 of its row's largest may be off by 2^-21 of that, as two e4m3
+    planes hold multiples of 2^-13 under a scale that puts the largest at 2^7 or more),
     a weight by that twice and the exponential's 4 u, the two sums by (keys + 64) u.  Then the weights'
     rounding.  fp32: three planes of 8 bits, 2^-26 of a weight.  bf16 calls: fp16, half a step of
     which is 2^-11 of a weight, or below fp16's normal numbers 2^-25, where the largest weight (with V's
@@ -174,6 +176,10 @@ def attend(shape, q, k_rows, v_rows, v_scales, table, kv_len, new_len):
             x = q[b, h, :n].double()
             logits = (x @ k.T * scale).masked_fill(~seen, -math.inf)
             off = (x.abs() @ k.abs().T * scale).masked_fill(~seen, 0.0).amax(1, keepdim=True) * (dh + 8) * u
+            if shape.dtype == "bf16":
+                top = x.abs().nan_to_num(0).amax(1, keepdim=True)
+                small = (x.abs() < 2.0 ** -13 * top) * top * 2.0 ** -21
+                off = off + (small @ k.abs().T * scale).masked_fill(~seen, 0.0).amax(1, keepdim=True)
             p = torch.where(seen.any(1, keepdim=True), torch.softmax(logits, 1), 0.0)
             out[b, h, :n] = p @ v
             s = torch.where(there, v_scales.double()[block, h // G], 0.0)

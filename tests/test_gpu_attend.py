@@ -350,3 +350,18 @@ def test_a_cache_of_more_than_32_bits():
     for a, b in zip(*outs):
         assert torch.equal(a, b)
     assert bool(outs[0][0].any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 40])
+def test_queries_of_wide_range(dtype, T):
+    """Entries from 2^-30 to 2^5 in a row, rows from 2^-40 to 2^10, and a row of zeros."""
+    import torch
+    shape = wl.CacheShape(dtype, 2, 4, 2, 128, 16, 30, 14, T)
+    q, cache, table, rows = make(shape, [200, 90], 21)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    e = torch.randint(-30, 6, q.shape, generator=g, device="cuda").double()
+    r = torch.randint(-40, 11, (2, 4, T, 1), generator=g, device="cuda").double()
+    q = (q.double() * torch.exp2(e + r)).clamp(-3e4, 3e4).to(q.dtype)
+    q[0, 0, 0] = 0
+    check(shape, q, cache, table, rows, [200, 90], None)

@@ -13,7 +13,7 @@
 // Softmax in one pass against a reference that is raised only where a lane's weights of a tile add up to more
 // than 2^12, so that most tiles need no exchange between lanes and no maximum.
 //
-// Two forms, by rows: up to 16, with 16x16x32 instructions and 64 keys at a time (bound by HBM: 2 dh
+// Two forms, by rows (`attend_form`): up to 16, with 16x16x32 instructions and 64 keys at a time (bound by HBM: 2 dh
 // bytes per token and kv head); more, 32 to a wave, with 32 keys at a time, two tiles in flight.  There a bf16
 // q goes into two e4m3 planes, which are multiplied with K as it is stored, 64 dims an instruction, and V is
 // converted for 32x32x16 instructions (bound by the vector unit beside the matrix pipe: per logit a multiply-add,
@@ -1080,9 +1080,11 @@ template <typename T, int DP>
 hipError_t launch_dp(const AttendArgs &a, hipStream_t s) {
     static std::atomic<uint64_t> few{0}, one{0}, two{0};
     const size_t acc = kWaves * DP * 16 * sizeof(float), refs = kWaves * sizeof(int);
-    const size_t lds = acc + kWaves * 32 * 2 * sizeof(float) + refs;
-    if (a.row_tiles == 2 && a.row_waves == 2) return launch_attend(attend_many_kernel<T, DP, 2>, a, lds, two, s);
-    if (a.row_tiles == 2) return launch_attend(attend_many_kernel<T, DP, 1>, a, lds, one, s);
+    if constexpr (attend_many_fits(sizeof(T) == 2, DP)) {
+        const size_t lds = acc + kWaves * 32 * 2 * sizeof(float) + refs;
+        if (a.row_tiles == 2 && a.row_waves == 2) return launch_attend(attend_many_kernel<T, DP, 2>, a, lds, two, s);
+        if (a.row_tiles == 2) return launch_attend(attend_many_kernel<T, DP, 1>, a, lds, one, s);
+    }
     return launch_attend(attend_few_kernel<T, DP>, a, acc + kWaves * 16 * 2 * sizeof(float) + refs, few, s);
 }
 

@@ -82,10 +82,13 @@ struct AttendArgs {
 constexpr int kAttendWaves = 4;
 // Keys that a wave takes at a time, by the tiles of 16 rows that it holds.
 constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
+constexpr bool attend_many_fits(bool is_bf16, int head_dim) { return is_bf16 || head_dim <= 192; }
 // How a call is cut into workgroups: fills the last five fields from the others.
 // A workgroup of the few-row kernel holds one tile of 16 rows, of the many-row kernel 32 rows a wave.  16
 // heads of 8 kv heads, 3000 keys, GPU time in us, few and many: 8 rows 19.8 and 20.7, 16 rows 19.6 and
-// 20.3, 20 rows (two tiles of 16) 21.7 and 20.6, 32 rows 25.5 and 22.5.
+// 20.3, 20 rows (two tiles of 16) 21.7 and 20.6, 32 rows 25.5 and 22.5.  In fp32 with heads above 192 the many-row
+// kernel would not fit the registers (4 x 4 kv heads, 1024 rows, 2000 keys 208 us, few rows at a time 106; at
+// 192 76 and 85).
 // Two of the many-row kernel's waves share their keys, each with rows of its own, where that leaves a
 // workgroup a CU: keys are read half as often, but walked by half the waves.  One and two row waves, by
 // the workgroups that two make:
@@ -103,8 +106,8 @@ inline void attend_form(AttendArgs &a) {
     constexpr int64_t kCus = 256;
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T, heads = (int64_t)a.B * a.Hkv;
     const int64_t pair = 4 * kCacheGroup;  // rows of two row waves
-    a.row_tiles = rows <= kCacheGroup ? 1 : 2;
-    a.row_waves = rows > 2 * kCacheGroup && heads * ((rows + pair - 1) / pair) >= kCus ? 2 : 1;
+    a.row_tiles = rows <= kCacheGroup || !attend_many_fits(a.is_bf16, a.dh) ? 1 : 2;
+    a.row_waves = a.row_tiles == 2 && rows > 2 * kCacheGroup && heads * ((rows + pair - 1) / pair) >= kCus ? 2 : 1;
     const int block = kCacheGroup * a.row_tiles * a.row_waves;
     a.row_blocks = (int)((rows + block - 1) / block);
     const int64_t units = heads * a.row_blocks;

@@ -149,8 +149,12 @@ def attend(shape, q, k_rows, v_rows, v_scales, table, kv_len, new_len):
     planes hold multiples of 2^-13 under a scale that puts the largest at 2^7 or more),
     a weight by that twice and the exponential's 4 u, the two sums by (keys + 64) u.  Then the weights'
     rounding.  fp32: three planes of 8 bits, 2^-26 of a weight.  bf16 calls: fp16, half a step of
-    which is 2^-11 of a weight, or below fp16's normal numbers 2^-25, where the largest weight (with V's
-    scale) that a wave meets is 2^4 or more: 2^-29 of the largest p s, times values of at most 448."""
+    which is 2^-11 of a weight, or below fp16's normal numbers 2^-25.  A value's scale s goes with the value
+    down to 2^-15 of the largest scale S, beyond that with the weight, so a weight's error of 2^-25 moves a sum
+    by at most 2^-25 448 S; and the reference is such that the largest p_j min(1, 2^15 s_j / S) of a wave's keys
+    is 2^4 or more.  Divided by that: 2^-29 448 S max_j(p_j min(1, 2^15 s_j / S)) a key.  (A wave whose own largest
+    scale is t < S: 2^-29 448 t max_j(p_j min(1, 2^15 s_j / t)), which is less, as t min(1, 2^15 s_j / t) =
+    min(t, 2^15 s_j) grows with t.)"""
     bs, T, G = shape.block_size, shape.n_new, shape.q_heads // shape.kv_heads
     dh, u = shape.head_dim, 2.0 ** -24
     scale = shape.scale if shape.scale > 0 else dh ** -0.5
@@ -184,5 +188,5 @@ def attend(shape, q, k_rows, v_rows, v_scales, table, kv_len, new_len):
             out[b, h, :n] = p @ v
             s = torch.where(there, v_scales.double()[block, h // G], 0.0)
             bound[b, h, :n] = ((p @ v.abs()) * (2 * off + (length + 72) * u + planes)
-                               + length * floor * (p * s).amax(1, keepdim=True))
+                               + length * floor * (p * torch.minimum(s.amax(), 2.0 ** 15 * s)).amax(1, keepdim=True))
     return out, bound

@@ -118,6 +118,12 @@ def test_large_logits_and_scales_far_apart():
         run(dtype, 4, 4, 64, 16, 1, [700, 65], spread=30, seed=8)
 
 
+@pytest.mark.parametrize("T,lens", [(33, [3005, 3025]), (1, [3005, 40]), (4, [300, 2000])])
+def test_scales_on_either_side_of_what_goes_with_the_values(T, lens):
+    """Scales 2^-27 .. 2^-7 in one sequence, and softmax near one key."""
+    run("bf16", 132 if T > 4 else 8, 4, 48, 16, T, lens, seed=50279, gain=4, spread=20)
+
+
 @pytest.mark.parametrize("apart", [12, 30, 90])
 @pytest.mark.parametrize("T", [1, 40])
 def test_all_weight_on_blocks_of_small_values(apart, T):

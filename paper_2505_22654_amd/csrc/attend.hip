@@ -250,11 +250,9 @@ __device__ __forceinline__ void load_query(const AttendArgs &a, const Row &row, 
 // both are exact for entries down to 2^-13 of the largest (lo's last place is 2^-13), and below it off by 2^-14 of
 // 2^e, 2^-21 of the largest.  The planes' 2^e and 2^(e - 4) are operands of the instruction (exponent bytes).
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ i32x8_t eight(const uint4 &a, const uint4 &b) {
     return i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
-}
-__device__ __forceinline__ uint32_t to_fp8(float a, float b, float c, float d) {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 // Row of a lane for products of 64 dims, 32 in each half of the wave: those that its 16-byte pieces of K are.
 template <int kN>
@@ -284,7 +282,7 @@ __device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &r
     const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -100), 120);
     scale[0] = e + 127;
     scale[1] = e + 127 - 4;
-    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    const float hi_unit = pow2(e), lo_unit = pow2(e - 4);
 #pragma unroll
     for (int m = 0; m < kN; ++m)
 #pragma unroll
@@ -293,16 +291,17 @@ __device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &r
             unpack16<bf16_t>(raw[m][i], f);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float x[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = f[4 * h + r] * inv;
-                const uint32_t w = to_fp8(x[0], x[1], x[2], x[3]);
-                x[0] -= __builtin_amdgcn_cvt_f32_fp8(w, 0);
-                x[1] -= __builtin_amdgcn_cvt_f32_fp8(w, 1);
-                x[2] -= __builtin_amdgcn_cvt_f32_fp8(w, 2);
-                x[3] -= __builtin_amdgcn_cvt_f32_fp8(w, 3);
-                out[m][0][2 * i + h] = (int)w;
-                out[m][1][2 * i + h] = (int)to_fp8(16.f * x[0], 16.f * x[1], 16.f * x[2], 16.f * x[3]);
+                const float *x = f + 4 * h;
+                i16x2_t w = {0, 0}, v = {0, 0};
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[0], x[1], hi_unit, false);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[2], x[3], hi_unit, true);
+                const int hi = __builtin_bit_cast(int, w);
+                const f32x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, hi_unit, false);
+                const f32x2_t up = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, hi_unit, true);
+                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, x[0] - lo[0], x[1] - lo[1], lo_unit, false);
+                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, x[2] - up[0], x[3] - up[1], lo_unit, true);
+                out[m][0][2 * i + h] = hi;
+                out[m][1][2 * i + h] = __builtin_bit_cast(int, v);
             }
         }
 }

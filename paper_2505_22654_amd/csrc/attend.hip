@@ -280,7 +280,7 @@ __device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &r
     top = fmaxf(top, __shfl_xor(top, 32, kWave));
     // 2^e with 128 <= top / 2^e < 256
     const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -100), 120);
-    scale[0] = e + 127;
+    scale[0] = top < INFINITY ? e + 127 : 255;  // (255: NaN, where the conversions would end at the largest number)
     scale[1] = e + 127 - 4;
     const float hi_unit = pow2(e), lo_unit = pow2(e - 4);
 #pragma unroll

@@ -371,3 +371,19 @@ def test_queries_of_wide_range(dtype, T):
     q = (q.double() * torch.exp2(e + r)).clamp(-3e4, 3e4).to(q.dtype)
     q[0, 0, 0] = 0
     check(shape, q, cache, table, rows, [200, 90], None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 40])
+def test_a_query_that_is_not_finite_spoils_its_row_alone(dtype, T):
+    import torch
+    shape = wl.CacheShape(dtype, 2, 6, 2, 128, 16, 30, 14, T)
+    q, cache, table, rows = make(shape, [200, 90], 5)
+    want, _ = check(shape, q, cache, table, rows, [200, 90], None)
+    odd = torch.zeros(q.shape[:3], dtype=torch.bool, device="cuda")
+    odd[0, 1, T - 1] = odd[1, 5, 0] = odd[1, 2, 1] = True
+    q[0, 1, T - 1, 3] = float("nan")
+    q[1, 5, 0, 100] = float("inf")
+    q[1, 2, 1, ::2] = -float("inf")
+    got = vb.cache_attend(shape, q, cache, table, i32([200, 90]))["out"]
+    assert torch.equal(got[~odd], want[~odd]) and bool(got[odd].isnan().all())

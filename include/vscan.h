@@ -489,8 +489,9 @@ int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v
  *               no key, are zero
  * A block number outside the cache stands for keys that are not there.  NaN in a
  * key or a value reaches the rows that see it and no others.  out must not overlap
- * an input.  Logits, softmax and sums are in 32 bits; in bf16 calls the weights are
- * multiplied in fp16, a row's largest as 2^4 or more.  VSCAN_ERR_UNSUPPORTED where the
+ * an input.  Logits, softmax and sums are in 32 bits; bf16 calls of more than 16 rows
+ * (Hq / Hkv) n_new multiply the weights in fp16 (2^-11 of each, the largest of a row as 2^4
+ * or more), calls of fewer rows to 2^-22.  VSCAN_ERR_UNSUPPORTED where the
  * blocks of 64 rows (16 in fp32 with head_dim > 192) of the (Hq / Hkv) n_new rows of all
  * sequences and kv heads reach 2^24.  Workspace:
  * vscan_cache_attend_workspace_size bytes, 16-byte aligned (0: none is needed, NULL is

@@ -5,9 +5,11 @@
 // takes them, so they never leave the registers.  The cache is stored in operand order: a lane's 16
 // bytes are one load, and nothing is staged in LDS.
 //
-// bf16 calls: K times q, both exact; V as fp16 (exact) times the weights in fp16 (2^-11 of each;
-// bf16's 2^-8 would add as much to the error as the result's own rounding).  fp32 calls: q and the
-// weights as three bf16 planes each, V as bf16.  K's scale goes into the logits; V's, a power of two,
+// bf16 calls: K times q, both exact; V as fp16 (exact) times the weights in fp16: in two planes for up to 16
+// rows, whose sum is a weight to 2^-22 (32 sequences of up to 3427 keys 126.1 us with one, 127.8 with two, bound by
+// memory), in one above, 2^-11 of each weight: a quarter of that is what is left in a sum of many keys, a tenth of
+// the result's own rounding, and the second plane's products would not hide (3 x 300 rows over 2604 keys 42
+// and 54 us, 8 x 512 over 4096 167 and 220).  fp32 calls: q and the weights as three bf16 planes each, V as bf16.  K's scale goes into the logits; V's, a power of two,
 // is taken relative to the largest that the wave has met: down to 2^-15 with the values, beyond that
 // with the weights, whose reference it then enters, so that the largest contributions keep their bits.
 // Softmax in one pass against a reference that is raised only where a lane's weights of a tile add up to more
@@ -63,7 +65,7 @@ template <>
 struct Operand<bf16_t> {
     typedef f16x8_t vec;
     typedef f16x2_t pair;
-    static constexpr int kPlanes = 1, kQueryPlanes = 1;
+    static constexpr int kFewPlanes = 2, kManyPlanes = 1, kQueryPlanes = 1;
     static __device__ __forceinline__ pair from_fp8(uint32_t w, float s, bool hi) {
         return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, false);
     }
@@ -78,7 +80,7 @@ template <>
 struct Operand<float> {
     typedef bf16x8_t vec;
     typedef bf16x2_t pair;
-    static constexpr int kPlanes = 3, kQueryPlanes = 3;
+    static constexpr int kFewPlanes = 3, kManyPlanes = 3, kQueryPlanes = 3;
     static __device__ __forceinline__ pair from_fp8(uint32_t w, float s, bool hi) {
         return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
     }
@@ -110,8 +112,8 @@ __device__ __forceinline__ void split(f32x2_t x, typename O::pair *out) {
     for (int p = 0; p < P; ++p) {
         out[p] = __builtin_convertvector(x, typename O::pair);
         if (p + 1 < P) {
-            x[0] -= (float)out[p][0];
-            x[1] -= (float)out[p][1];
+            x[0] = fmaf((float)out[p][0], -1.f, x[0]);  // (one instruction, from a half)
+            x[1] = fmaf((float)out[p][1], -1.f, x[1]);
         }
     }
 }
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     constexpr int kTile = attend_tile(1), kGroups = kTile / kCacheGroup;
     constexpr int kH = DP / 64;  // 16-byte loads per lane and group
     constexpr int kD = DP / 16;  // tiles of 16 dims
-    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes, step = kTile * kWaves;
+    constexpr int kQ = O::kQueryPlanes, kP = O::kFewPlanes, step = kTile * kWaves;
     extern __shared__ float4 lds4[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -605,7 +607,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
         fetch(a.k_cache, next, kb);
 
-        Scales<kGroups, kP == 1> sc;
+        Scales<kGroups, sizeof(T) == 2> sc;
         sc.of(at[0], eref);
         settle_products<8>();
         typename O::vec pb[kGroups / 2][kP];
@@ -746,7 +748,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     constexpr bool kOdd = DP % 128 != 0;        // and a last 64 dims: half a piece
     constexpr int kD = DP / 32;                 // tiles of 32 dims
     constexpr int kKeyWaves = kWaves / kRowWaves;  // waves that share rows
-    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes, step = kTile * kKeyWaves;
+    constexpr int kQ = O::kQueryPlanes, kP = O::kManyPlanes, step = kTile * kKeyWaves;
     extern __shared__ float4 lds4[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave % kKeyWaves, row_wave = wave / kKeyWaves;
@@ -853,7 +855,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
         fetch_keys(next, kb);
 
-        Scales<kGroups, kP == 1> sc;
+        Scales<kGroups, sizeof(T) == 2> sc;
         sc.of(at, eref);
         settle_products<8>();
         typename O::vec pb[kGroups][kP];

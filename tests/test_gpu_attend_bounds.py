@@ -1,0 +1,67 @@
+"""vscan_cache_attend where its arithmetic could go wrong: sums that cancel, logits and queries at the ends
+of fp32's range, queries with entries far apart, and every compiled form.  Definition and bounds as in
+`decode_reference.attend`."""
+import pytest
+
+from paper_2505_22654_amd import binding as vb
+from paper_2505_22654_amd import workloads as wl
+from tests import decode_reference as ref
+from tests.test_gpu_attend import HALF_STEP, i32, make
+
+pytestmark = pytest.mark.gpu
+
+
+def _stored(shape, k, v, lens):
+    """A cache with the rows of k and v [B,Hkv,L,dh], its table, and the rows as the cache holds them."""
+    import dataclasses
+
+    import torch
+    B, L = shape.batch, k.shape[2]
+    cache = vb.cache_alloc(shape)
+    for n in "kv":
+        cache[n].zero_()
+        cache[n + "_scale"].fill_(1.0)
+    per = -(-L // shape.block_size)
+    assert per <= shape.max_blocks and B * per <= shape.n_blocks
+    table = torch.full((B, shape.max_blocks), -1, dtype=torch.int32, device="cuda")
+    new = dataclasses.replace(shape, n_new=L, max_len=0)
+    plan = vb.cache_plan(new, i32([0] * B), i32(lens), i32(list(range(shape.n_blocks))), i32([0]), table)
+    vb.cache_store(new, k, v, plan["slot_map"], cache)
+    rows = {n: (ref.read(cache, shape, n) * cache[n + "_scale"].double()[..., None, None])[..., :shape.head_dim]
+            for n in "kv"}
+    return cache, table, rows
+
+
+def _few_rows_bound(shape, q, rows, cache, table, lens):
+    """(result, bound) in 64 bits of a bf16 call of at most 16 rows: what fp32 calls are held to, for three
+    planes of 8 bits 2^-26 of a weight, and for two planes of fp16 in their place half a step of the second,
+    2^-22 of a weight, or below fp16's normal numbers 2^-25, of a largest weight of 2^4: 2^-29 of values of at
+    most 448 scales a key."""
+    import dataclasses
+    f32 = dataclasses.replace(shape, dtype="f32")
+    want, bound = ref.attend(f32, q, rows["k"], rows["v"], cache["v_scale"], table, lens, None)
+    size, _ = ref.attend(f32, q, rows["k"], rows["v"].abs(), cache["v_scale"], table, lens, None)
+    return want, bound + 2.0 ** -22 * size + max(lens) * 448 * 2.0 ** -29 * float(cache["v_scale"].max())
+
+
+@pytest.mark.parametrize("hq,hkv,dh,T,length", [(4, 4, 128, 1, 40), (28, 4, 128, 1, 333), (8, 2, 64, 3, 65), (2, 1, 192, 8, 20),
+                                               (16, 1, 256, 1, 700), (6, 3, 80, 1, 5000)])
+def test_sums_that_cancel_keep_their_bits_in_few_rows(hq, hkv, dh, T, length):
+    """Tokens in pairs of opposite values and of nearly the same weight: what is left is far below the
+    parts, and the weights' rounding would show (2^-11 of the parts against the bound's 2^-18)."""
+    import torch
+    B = 2
+    shape = wl.CacheShape("bf16", B, hq, hkv, dh, 16, 2 * (-(-length // 16)) + 1, -(-length // 16), T)
+    g = torch.Generator(device="cuda").manual_seed(length)
+    k = torch.randn((B, hkv, length, dh), generator=g, device="cuda").bfloat16()
+    v = torch.randn((B, hkv, length, dh), generator=g, device="cuda").bfloat16()
+    pairs = length // 2
+    v[:, :, 1:2 * pairs:2] = -v[:, :, 0:2 * pairs:2]
+    v[:, :, 2 * pairs:] = 0
+    lens = [length, length - 1 if length % 2 else length]
+    cache, table, rows = _stored(shape, k, v, lens)
+    q = (torch.randn((B, hq, T, dh), generator=g, device="cuda") * 0.01).bfloat16()
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    want, bound = _few_rows_bound(shape, q, rows, cache, table, lens)
+    over = (got.double() - want).abs() - bound - HALF_STEP["bf16"] * want.abs()
+    assert float(over.max()) <= 0, (shape, float(over.max()))

@@ -99,11 +99,12 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a, in
     }
 }
 
-constexpr int kTableThreads = 256;
 __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(PlanArgs a, int row_parts) {
     const int b = blockIdx.x / row_parts, part = blockIdx.x % row_parts;
     const Request q = {a.requests[4 * b], a.requests[4 * b + 1], a.requests[4 * b + 2]};
-    for (int r = part * kTableThreads + threadIdx.x; r < a.n_new; r += row_parts * kTableThreads) write_row(a, b, q, r);
+    // (unsigned: the last step goes past n_new by a quarter of it)
+    for (uint32_t r = part * kTableThreads + threadIdx.x; r < (uint32_t)a.n_new; r += row_parts * kTableThreads)
+        write_row(a, b, q, (int)r);
 }
 
 // ---- new keys and values -----------------------------------------------------------------------
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(StoreArgs a,
 
 template <typename T, int DP, int LANES, int kHold>
 hipError_t launch_store_as(const StoreArgs &a, hipStream_t s) {
-    const int runs = (a.n_new + (1 << a.block_shift) - 2) / (1 << a.block_shift) + 1;
+    const int runs = (int)store_runs(a.n_new, 1 << a.block_shift);
     const int pages = 2 * a.B * a.Hkv * runs, per = kStoreThreads / LANES;
     hipLaunchKernelGGL((cache_store_kernel<T, DP, LANES, kHold>), dim3((pages + per - 1) / per), dim3(kStoreThreads), 0,
                        s, a, runs, pages);
@@ -451,7 +452,7 @@ hipError_t launch_cache_plan(const void *args, hipStream_t s) {
 
 hipError_t launch_cache_tables(const void *args, hipStream_t s) {
     const PlanArgs &a = *static_cast<const PlanArgs *>(args);
-    const int parts = (a.n_new + kTableThreads * 4 - 1) / (kTableThreads * 4);
+    const int parts = plan_table_parts(a.n_new);
     hipLaunchKernelGGL(cache_tables_kernel, dim3(a.B * parts), dim3(kTableThreads), 0, s, a, parts);
     return hipGetLastError();
 }

@@ -50,6 +50,9 @@ inline int plan_workgroups(const PlanArgs &a) {
 }
 // Whether `requests` may be written: not where one launch holds them in LDS whatever overlaps.
 inline bool plan_needs_scratch(int64_t B, int64_t n_new) { return B > kPlanThreads || B * n_new > kPlanAlone; }
+// Workgroups of a request where a second launch writes the tables.  (n_new may be anything below 2^31.)
+constexpr int kTableThreads = 256;
+inline int plan_table_parts(int n_new) { return (int)(((int64_t)n_new + kTableThreads * 4 - 1) / (kTableThreads * 4)); }
 hipError_t launch_cache_plan(const void *args, hipStream_t s);
 hipError_t launch_cache_tables(const void *args, hipStream_t s);
 
@@ -65,6 +68,8 @@ struct StoreArgs {
 // 32 32.7 and 44.8, of 64 36.0 and 33.1, of 128 45.3 and 34.1; one token 4.1 and 4.7 in any, but a wave takes
 // long to fill or rescale a large page.
 constexpr int store_pages(int block_size) { return block_size <= 32 ? 4 : 1; }
+// Blocks that n_new rows of a sequence can touch.
+constexpr int64_t store_runs(int64_t n_new, int block_size) { return (n_new + block_size - 2) / block_size + 1; }
 hipError_t launch_cache_store(const void *args, hipStream_t s);
 
 struct AttendArgs {

@@ -222,7 +222,7 @@ int cache_store(const vscan_cache_desc *d, const void *k, const void *v, const i
     const int rc = check_cache(d);
     if (rc != VSCAN_OK) return rc;
     // one wave or workgroup per (k or v, sequence, kv head, block that the new rows touch)
-    const int64_t runs = (d->n_new + d->block_size - 2) / d->block_size + 1;
+    const int64_t runs = store_runs(d->n_new, d->block_size);
     if ((int64_t)d->batch * d->kv_heads * runs * 2 >= kMaxWorkgroups * store_pages(d->block_size)) return VSCAN_ERR_UNSUPPORTED;
     if (d->batch == 0 || d->n_new == 0) return VSCAN_OK;
     if (!k || !v || !slot_map || !k_cache || !v_cache || !k_scale || !v_scale) return VSCAN_ERR_NULL;

@@ -118,16 +118,6 @@ __device__ __forceinline__ void split(f32x2_t x, typename O::pair *out) {
     }
 }
 
-// Waits until the last register of a product is there for the vector unit.  (The wait states that the
-// compiler leaves by itself, 12 after a 32x32x16, were one tile in some too few where it went on to read
-// an accumulator from its last register: dims 123 and 127 of a row were wrong by a late product.)
-template <int kStates>
-__device__ __forceinline__ void settle_products() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_nop %0" ::"n"(kStates - 1));
-    __builtin_amdgcn_sched_barrier(0);
-}
-
 // Exponent of a power of two.
 __device__ __forceinline__ int exp_of(float s) {
     const int e = (int)(__float_as_uint(s) >> 23 & 255u) - 127;
@@ -609,7 +599,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 
         Scales<kGroups, sizeof(T) == 2> sc;
         sc.of(at[0], eref);
-        settle_products<8>();
+        __builtin_amdgcn_sched_barrier(0);
         typename O::vec pb[kGroups / 2][kP];
         float sums[kGroups];
         auto logit = [&](int u, int r, float add) {
@@ -689,10 +679,10 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
         fetch(a.v_cache, next, vb);
         at[0] = next;
-        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<16>();  // (accumulators that are copied for the next tile)
+        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<4>();  // (accumulators that are copied for the next tile)
     });
 
-    settle_products<16>();
+    settle_products<4>();
     if (nan_from < w.k1) {
         for (int kt = nan_from; kt < w.k1; kt += step) {
             TileAt<kGroups> t;
@@ -706,7 +696,6 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                 for (int d = 0; d < kD; ++d) {
                     const uint32_t w0 = word(vb[2 * v][d >> 2], d & 3), w1 = word(vb[2 * v + 1][d >> 2], d & 3);
                     const f32x4_t count = O::mfma(ones_at<O>(w0, w1), seen, f32x4_t{0.f, 0.f, 0.f, 0.f});
-                    settle_products<8>();
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[d][r] = count[r] > 0.f ? NAN : acc[d][r];
                 }
@@ -857,7 +846,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 
         Scales<kGroups, sizeof(T) == 2> sc;
         sc.of(at, eref);
-        settle_products<8>();
+        __builtin_amdgcn_sched_barrier(0);
         typename O::vec pb[kGroups][kP];
         float sums[kGroups];
         auto logit = [&](int r, float add) {
@@ -939,10 +928,10 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         }
         fetch_values(next, vb);
         at = next;
-        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<16>();
+        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<4>();
     });
 
-    settle_products<16>();
+    settle_products<4>();
     if (nan_from < w.k1) {
         for (int kt = nan_from; kt < w.k1; kt += step) {
             TileAt<kGroups> at;
@@ -961,7 +950,6 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) count[r] = 0.f;
                     count = O::mfma32(ones_at<O>(w0, w1), seen, count);
-                    settle_products<16>();
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[d][r] = count[r] > 0.f ? NAN : acc[d][r];
                 }

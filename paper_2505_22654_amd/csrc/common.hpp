@@ -200,6 +200,20 @@ __device__ __forceinline__ void mma32_chunk<float>(f32x16_t &acc, const uint4 &a
                                                0, 0);
 }
 
+// Wait states for products that are under way at the end of a block of the control flow.  A product's
+// registers may be used some states after it is issued (12 for a 32x32x16 in bf16), which nothing but the code
+// ensures.  Within a block the compiler does; over its end it can leave too few: it counts an unconditional
+// branch that stands behind a conditional one also where the conditional one is taken, and a block that it has
+// come to over a long way it does not look through again over a short one.  (At the top of a loop the last register
+// of an accumulator was read 11 states after the 32x32x16 product at its end, and was wrong.)  These states are
+// not counted by it: they stand in addition to its own.
+template <int kStates>
+__device__ __forceinline__ void settle_products() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop %0" ::"n"(kStates - 1));
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 __device__ __forceinline__ int acc_row(int r) {
     return 8 * (r >> 2) + 4 * (lane_id() >> 5) + (r & 3);
 }

@@ -329,6 +329,7 @@ __global__ __launch_bounds__(256, 2) void mean_lse_kernel(const T *__restrict__ 
                 const uint4 a = *reinterpret_cast<const uint4 *>(arow + 32 * c);
                 mma32_chunk<T>(acc, a, qfrag[c]);
             }
+            settle_products<2>();
             // acc[r] = q_row(lane%32) . k_(key0 + acc_row(r)); mask the ragged tail
             const int key0 = t * kMeanTile + sub * 32;
             if (key0 + 32 > n_keys) {
@@ -973,6 +974,7 @@ __global__ __launch_bounds__(256, MeanForm<T>::kWorkgroupsPerCu) void mean_pipe_
                     if (s + 2 < nstages) stage_load(s + 2);
                 }
                 step(t0 + j, acc[j & 1], acc[(j + 1) & 1], no{}, nothing);
+                settle_products<4>();
             }
         });
     }

@@ -168,6 +168,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave, (DEPTH == 2 && NC <= 4 && NRB 
             f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < NC; ++c) mma16_chunk<T>(acc, kf[c], qfrag[rb][c]);
+            if constexpr (NRB > 1) settle_products<4>();
             // acc[r]: key key0 + 4g + r, query row rb*16 + l16
             const int row = rb * 16 + l16;
             if (row < R) {

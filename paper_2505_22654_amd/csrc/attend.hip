@@ -34,6 +34,7 @@
 // tile these four took 177, 328, 117 and 44.  More rows a wave (64: 280 us where 32 took 179), eight waves (245)
 // and rows over all four waves (203) lost to this split.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 
@@ -53,7 +54,7 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = kAttendWaves;
-constexpr float kNothing = -1e30f;  // reference of a row that has seen no key
+constexpr float kNothing = -FLT_MAX;  // reference of a row that has seen no key: below every finite logit
 constexpr float kBias = 4.f;        // the largest weight is 2^4 when the reference is set ..
 constexpr float kRaise = 4096.f;    // .. and a lane's sum of a tile at most this until it is raised (fp16 holds 2^16)
 constexpr int kValueExp = -15;      // e4m3's 2^-9 times 2^-15 is fp16's smallest number

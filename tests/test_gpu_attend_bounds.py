@@ -65,3 +65,30 @@ def test_sums_that_cancel_keep_their_bits_in_few_rows(hq, hkv, dh, T, length):
     want, bound = _few_rows_bound(shape, q, rows, cache, table, lens)
     over = (got.double() - want).abs() - bound - HALF_STEP["bf16"] * want.abs()
     assert float(over.max()) <= 0, (shape, float(over.max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 3, 40])
+@pytest.mark.parametrize("length", [1, 70, 3000])
+def test_logits_far_below_zero(dtype, T, length):
+    """Every logit between -1.4e36 and -2e31.  One token, which every row sees that sees any, has half the others':
+    its value is the result."""
+    import torch
+    shape = wl.CacheShape(dtype, 2, 4, 2, 64, 16, 420, 200, T)
+    g = torch.Generator(device="cuda").manual_seed(length)
+    dt = vb._torch_dtype(dtype)
+    k = torch.full((2, 2, length, 64), -64.0, device="cuda")
+    first = max(length - T, 0)
+    k[:, :, first] = -32.0
+    v = torch.randn((2, 2, length, 64), generator=g, device="cuda").to(dt)
+    lens = [length, length]
+    cache, table, rows = _stored(shape, k.to(dt), v, lens)
+    at = table.long()[:, first // 16]
+    want = rows["v"][at, :, first % 16]                                    # [B, Hkv, dh]
+    for gain in (2.0 ** 96, 2.0 ** 111):
+        # 64 products of 32 gain or 64 gain, over 8: -256 gain and -512 gain
+        q = torch.full((2, 4, T, 64), gain, device="cuda").to(dt)
+        got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"].double()
+        seen = got[:, :, max(T - length, 0):]
+        assert bool((seen == want.repeat_interleave(2, 1)[:, :, None].to(dt).double()).all()), (gain, seen)
+        assert not got[:, :, :max(T - length, 0)].any()

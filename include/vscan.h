@@ -488,7 +488,8 @@ int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v
  *   out         DEVICE [B, Hq, n_new, dh]; rows t >= new_len[b], and rows that see
  *               no key, are zero
  * A block number outside the cache stands for keys that are not there.  NaN in a
- * key or a value reaches the rows that see it and no others.  out must not overlap
+ * key or a value reaches the rows that see it and no others; infinities and NaN in a
+ * query make its row NaN if it sees a key, and no other.  out must not overlap
  * an input.  Logits, softmax and sums are in 32 bits; bf16 calls of more than 16 rows
  * (Hq / Hkv) n_new multiply the weights in fp16 (2^-11 of each, the largest of a row as 2^4
  * or more), calls of fewer rows to 2^-22.  VSCAN_ERR_UNSUPPORTED where the

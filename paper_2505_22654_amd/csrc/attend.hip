@@ -471,6 +471,24 @@ __device__ __forceinline__ typename O::vec seen_keys(int lo, int hi, int lim) {
     return r;
 }
 
+// A sum of 0 is that of a row without keys, unless the row sees some and each logit is minus infinity (an
+// infinite query whose products have one sign): softmax has no value there, and the row is NaN.  Such a chunk's
+// reference is the number above kNothing; other chunks may still have keys with weight, so the last to join decides.
+constexpr float kHollow = -0x1.fffffcp127f;
+static_assert(kHollow > kNothing, "");
+// Whether a row that sees `lim` keys sees one of the workgroup's chunk.  (Its place is worked out again: kept
+// through the loop over the keys it cost heads of 256 2.5 % of their time.)
+__device__ __forceinline__ bool sees_any(const AttendArgs &a, int lim) {
+    int id = blockIdx.x;
+    asm volatile("" : "+s"(id));
+    const int32_t *table = a.block_table + (int64_t)(id / a.chunks / a.row_blocks / a.Hkv) * a.max_blocks;
+    const int k0 = id % a.chunks * a.chunk, k1 = min(k0 + a.chunk, lim);
+    bool any = false;
+    for (int key = k0; key < k1 && !any; key += 1 << a.block_shift)
+        any = (unsigned)table[key >> a.block_shift] < (unsigned)a.n_blocks;
+    return any;
+}
+
 // The results of the waves of a workgroup for a lane's row, from (reference, sum) pairs and scale
 // references in LDS: factors of their accumulators, and what the row has in all.
 template <int kN>
@@ -478,26 +496,31 @@ struct Joined {
     float f[kN], mx, sum, unit;
 };
 template <int kN>
-__device__ __forceinline__ Joined<kN> join_waves(const float *stat, const int *refs, int rows, int j, bool padding) {
+__device__ __forceinline__ Joined<kN> join_waves(const AttendArgs &a, const Row &row, const float *stat, const int *refs,
+                                                 int rows, int j) {
     Joined<kN> r;
     int e = kScaleExpMin;
     r.mx = kNothing;
     r.sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kN; ++w) {
-        r.mx = fmaxf(r.mx, stat[(w * rows + j) * 2]);
-        e = max(e, refs[w]);
+    for (int v = 0; v < kN; ++v) {
+        r.mx = fmaxf(r.mx, stat[(v * rows + j) * 2]);
+        e = max(e, refs[v]);
     }
 #pragma unroll
-    for (int w = 0; w < kN; ++w) {
-        r.f[w] = __builtin_amdgcn_exp2f(stat[(w * rows + j) * 2] - r.mx);
-        r.sum += r.f[w] * stat[(w * rows + j) * 2 + 1];
+    for (int v = 0; v < kN; ++v) {
+        r.f[v] = __builtin_amdgcn_exp2f(stat[(v * rows + j) * 2] - r.mx);
+        r.sum += r.f[v] * stat[(v * rows + j) * 2 + 1];
     }
     // a row without keys, or past new_len, is zero
-    const float inv = r.sum > 0.f && !padding ? 1.f / r.sum : 0.f;
+    const float inv = r.sum > 0.f && !row.padding ? 1.f / r.sum : 0.f;
 #pragma unroll
-    for (int w = 0; w < kN; ++w) r.f[w] *= inv * pow2(refs[w] - e);
+    for (int v = 0; v < kN; ++v) r.f[v] *= inv * pow2(refs[v] - e);
     r.unit = pow2(e);
+    if (__builtin_expect(__any(r.sum == 0.f), 0) && r.sum == 0.f && sees_any(a, row.lim)) {
+        if (a.chunks == 1) r.unit = NAN;
+        r.mx = kHollow;
+    }
     return r;
 }
 // Four dims of a row: `at` are the waves' accumulators, `stride` apart.
@@ -715,7 +738,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     }
     if (lane == 0) refs[wave] = eref;
     __syncthreads();
-    const Joined<kWaves> jn = join_waves<kWaves>(stat, refs, 16, j, row.padding);
+    const Joined<kWaves> jn = join_waves<kWaves>(a, row, stat, refs, 16, j);
 #pragma unroll
     for (int i = 0; i < kD / kWaves; ++i) {
         const int d = i * kWaves + wave;
@@ -979,7 +1002,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                 lds4[((wave * kHalf + i) * 4 + q) * kWave + lane] = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
             }
         __syncthreads();
-        if (half == 0) jn = join_waves<kKeyWaves>(stat + row_wave * kKeyWaves * 64, refs + row_wave * kKeyWaves, 32, j, row.padding);
+        if (half == 0) jn = join_waves<kKeyWaves>(a, row, stat + row_wave * kKeyWaves * 64, refs + row_wave * kKeyWaves, 32, j);
 #pragma unroll
         for (int i = 0; i < kHalf; ++i)
 #pragma unroll
@@ -1051,7 +1074,7 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a) 
         for (int e = 0; e < 4; ++e) o[e] = o[e] * f + __shfl_xor(o[e], d, kWave) * fo;
     }
     if (lane >= kLanes || dim >= a.dh) return;
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = sum > 0.f ? 1.f / sum : mx == kHollow ? NAN : 0.f;
     const int64_t at = (((int64_t)b * a.Hq + hk * G + (r - t * G)) * a.T + t) * a.dh + dim;
     store4<T>(static_cast<T *>(a.out) + at, o * inv);
 }

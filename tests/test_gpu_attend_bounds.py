@@ -92,3 +92,33 @@ def test_logits_far_below_zero(dtype, T, length):
         seen = got[:, :, max(T - length, 0):]
         assert bool((seen == want.repeat_interleave(2, 1)[:, :, None].to(dt).double()).all()), (gain, seen)
         assert not got[:, :, :max(T - length, 0)].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 3, 40])
+@pytest.mark.parametrize("length,present", [(1, True), (70, True), (3000, True), (70, False)])
+def test_an_infinite_query_is_nan_also_where_every_logit_is_minus_infinity(dtype, T, length, present):
+    """Keys of one sign in the dim where the query is infinite; rows without a key stay zero, the others as
+    they are."""
+    import torch
+    shape = wl.CacheShape(dtype, 2, 4, 2, 64, 16, 420, 200, T)
+    g = torch.Generator(device="cuda").manual_seed(length)
+    k = torch.randn((2, 2, length, 64), generator=g, device="cuda")
+    k[..., 5] = 0.5 + k[..., 5].abs()
+    k, v = k.to(vb._torch_dtype(dtype)), torch.randn((2, 2, length, 64), generator=g, device="cuda").to(vb._torch_dtype(dtype))
+    lens = [length, 0]
+    cache, table, rows = _stored(shape, k, v, lens)
+    if not present:
+        table.fill_(-1)
+    q = torch.randn((2, 4, T, 64), generator=g, device="cuda").to(vb._torch_dtype(dtype))
+    want = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    q[:, 1, T - 1, 5] = -float("inf")
+    q[:, 2, 0, 5] = -float("inf")
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    odd = torch.zeros((2, 4, T), dtype=torch.bool, device="cuda")
+    if present:
+        odd[0, 1, T - 1] = True
+        odd[0, 2, 0] = length >= T
+    assert torch.equal(got[~odd], want[~odd]) and not want.isnan().any()
+    assert bool(got[odd].isnan().all())
+    assert not got[1].any() and (present or not got.any())

@@ -490,7 +490,8 @@ int vscan_cache_store(const vscan_cache_desc *desc, const void *k, const void *v
  * A block number outside the cache stands for keys that are not there.  NaN in a
  * key or a value reaches the rows that see it and no others; infinities and NaN in a
  * query make its row NaN if it sees a key, and no other.  out must not overlap
- * an input.  Logits, softmax and sums are in 32 bits; bf16 calls of more than 16 rows
+ * an input.  Logits, softmax and sums are in 32 bits (a logit above their range makes its
+ * row NaN, below it the key has no weight); bf16 calls of more than 16 rows
  * (Hq / Hkv) n_new multiply the weights in fp16 (2^-11 of each, the largest of a row as 2^4
  * or more), calls of fewer rows to 2^-22.  VSCAN_ERR_UNSUPPORTED where the
  * blocks of 64 rows (16 in fp32 with head_dim > 192) of the (Hq / Hkv) n_new rows of all

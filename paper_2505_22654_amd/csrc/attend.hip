@@ -209,22 +209,59 @@ __device__ __forceinline__ Row row_of(const AttendArgs &a, const Work &w, int r)
     return x;
 }
 
-// Eight entries of a query as planes.
+// Queries at the top of the range.  K goes into the products without its scale, so up to 256 products of 448 and an
+// entry of kFar stay inside fp32; where an entry of a wave's rows is larger, they are all taken by 2^-24, which
+// the factor of the logits makes up for (c above 2^127 then: infinite logits, and NaN).
+constexpr float kFar = 0x1p104f, kNear = 1.f / kFarScale;
+// Eight entries of a query.
 template <typename T>
-__device__ __forceinline__ void load_query(const AttendArgs &a, const Row &row, int d, bf16x8_t *out) {
-    const bool ok = row.at >= 0 && !row.padding && d < a.dh;
-    const T *src = static_cast<const T *>(a.q) + max(row.at, (int64_t)0);
+struct QueryPiece {
+    uint4 raw[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const AttendArgs &a, const Row &row, int d) {
+        const bool ok = row.at >= 0 && !row.padding && d < a.dh;
+        const T *src = static_cast<const T *>(a.q) + max(row.at, (int64_t)0);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = load16_guard(src, (int64_t)d * (int)sizeof(T) + 16 * i, ok);
+    }
+    __device__ __forceinline__ void get(float *f) const {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) unpack16<T>(raw[i], f + i * ElemTraits<T>::kPer16B);
+    }
+    __device__ __forceinline__ float largest() const {
+        float f[8], top = 0.f;
+        get(f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+        return top;
+    }
+    __device__ __forceinline__ void come_near() {
+        float f[8];
+        get(f);
+        if constexpr (sizeof(T) == 2) {
+            union {
+                __bf16 h[8];
+                uint4 u;
+            } o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o.h[e] = (__bf16)(f[e] * kNear);
+            raw[0] = o.u;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                raw[i] = make_uint4(__float_as_uint(f[4 * i] * kNear), __float_as_uint(f[4 * i + 1] * kNear),
+                                    __float_as_uint(f[4 * i + 2] * kNear), __float_as_uint(f[4 * i + 3] * kNear));
+        }
+    }
+    // as planes of bf16
+    __device__ __forceinline__ void planes(bf16x8_t *out) const;
+};
+template <typename T>
+__device__ __forceinline__ void QueryPiece<T>::planes(bf16x8_t *out) const {
     if constexpr (sizeof(T) == 2) {
-        union {
-            uint4 u;
-            bf16x8_t v;
-        } raw;
-        raw.u = load16_guard(src, (int64_t)d * 2, ok);
-        out[0] = raw.v;
+        out[0] = __builtin_bit_cast(bf16x8_t, raw[0]);
     } else {
         float f[8];
-        unpack16<float>(load16_guard(src, (int64_t)d * 4, ok), f);
-        unpack16<float>(load16_guard(src, (int64_t)d * 4 + 16, ok), f + 4);
+        get(f);
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             bf16x2_t p[3];
@@ -237,6 +274,19 @@ __device__ __forceinline__ void load_query(const AttendArgs &a, const Row &row, 
         }
     }
 }
+// Whether one of the wave's rows is too large as it is; if so they are all scaled.
+template <typename T, int kN>
+__device__ __forceinline__ bool come_near(QueryPiece<T> (&q)[kN]) {
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < kN; ++c) top = fmaxf(top, q[c].largest());
+    const bool far = __any(top >= kFar && top < INFINITY);
+    if (__builtin_expect(far, 0)) {
+#pragma unroll
+        for (int c = 0; c < kN; ++c) q[c].come_near();
+    }
+    return far;
+}
 
 // A bf16 query in two e4m3 planes, for products with K as it is stored: 2^e of a row puts its largest entry
 // at 2^7 to 2^8, hi = q / 2^e rounded to 4 bits, lo = 16 (q / 2^e - hi).  bf16's 8 bits leave lo at most 4, so
@@ -248,8 +298,9 @@ __device__ __forceinline__ i32x8_t eight(const uint4 &a, const uint4 &b) {
     return i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
 // Row of a lane for products of 64 dims, 32 in each half of the wave: those that its 16-byte pieces of K are.
+// Returns whether they are scaled by kNear (which their exponents hold).
 template <int kN>
-__device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &row, int g, i32x8_t (*out)[2], int *scale) {
+__device__ __forceinline__ bool load_query_fp8(const AttendArgs &a, const Row &row, int g, i32x8_t (*out)[2], int *scale) {
     const bool ok = row.at >= 0 && !row.padding;
     const bf16_t *src = static_cast<const bf16_t *>(a.q) + max(row.at, (int64_t)0);
     uint4 raw[kN][4];
@@ -272,9 +323,11 @@ __device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &r
         }
     top = fmaxf(top, __shfl_xor(top, 32, kWave));
     // 2^e with 128 <= top / 2^e < 256
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -100), 120);
-    scale[0] = top < INFINITY ? e + 127 : 255;  // (255: NaN, where the conversions would end at the largest number)
-    scale[1] = e + 127 - 4;
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -96), 120);
+    const bool far = __any(top >= kFar && top < INFINITY);
+    const int unit = e + 127 - (far ? 24 : 0);
+    scale[0] = top < INFINITY ? unit : 255;  // (255: NaN, where the conversions would end at the largest number)
+    scale[1] = unit - 4;
     const float hi_unit = pow2(e), lo_unit = pow2(e - 4);
 #pragma unroll
     for (int m = 0; m < kN; ++m)
@@ -297,6 +350,7 @@ __device__ __forceinline__ void load_query_fp8(const AttendArgs &a, const Row &r
                 out[m][1][2 * i + h] = __builtin_bit_cast(int, v);
             }
         }
+    return far;
 }
 
 // The keys of a tile: where its groups of 16 lie, and their scales.
@@ -317,6 +371,7 @@ struct Walk {
     const int32_t *table;
     int hk, step, k1, batch_kt, located = 0, block_ahead, lane_block, lane_e;
     float lane_c;
+    bool far = false;  // queries are scaled by kNear
 
     __device__ __forceinline__ Walk(const AttendArgs &args, int b, int hk_, int step_, int kt)
         : a(args), table(args.block_table + (int64_t)b * args.max_blocks), hk(hk_), step(step_), batch_kt(kt) {
@@ -341,7 +396,7 @@ struct Walk {
     }
     // (waited for at once, so that no later load of the loop is)
     __device__ __forceinline__ void settle() {
-        lane_c *= a.scale;
+        lane_c *= far ? a.far_scale : a.scale;
         lane_e = lane_block >= 0 ? exp_of(__int_as_float(lane_e)) : kScaleExpMin;
         asm volatile("" ::"v"(block_ahead));
     }
@@ -379,9 +434,10 @@ struct Walk {
             at.e[u] = __builtin_amdgcn_readlane(lane_e, tile * kGroups + u);
         }
     }
-    // The first kStages tiles: their keys and values are requested before their scales have come.
-    template <int kStages, typename Fetch>
-    __device__ __forceinline__ void begin(int kt, int end, TileAt<kGroups> *ats, Fetch fetch) {
+    // The first kStages tiles: their keys and values are requested before their scales, and what `far` looks
+    // at, the queries, have come.
+    template <int kStages, typename Fetch, typename Far>
+    __device__ __forceinline__ void begin(int kt, int end, TileAt<kGroups> *ats, Fetch fetch, Far is_far) {
         k1 = end;
         next_batch();
 #pragma unroll
@@ -389,6 +445,7 @@ struct Walk {
             locate(kt + i * step, ats[i]);
             fetch(i);
         }
+        far = is_far();
         settle();
 #pragma unroll
         for (int i = 0; i < kStages; ++i) scales_of(i, ats[i]);
@@ -573,9 +630,9 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     if (a.chunks > 1 && w.k0 >= w.reach) return;
 
     const Row row = row_of(a, w, w.row0 + j);
-    bf16x8_t qf[2 * kH][kQ];
+    QueryPiece<T> queries[2 * kH];
 #pragma unroll
-    for (int c = 0; c < 2 * kH; ++c) load_query<T>(a, row, (c >> 1) * 64 + g * 16 + (c & 1) * 8, qf[c]);
+    for (int c = 0; c < 2 * kH; ++c) queries[c].load(a, row, (c >> 1) * 64 + g * 16 + (c & 1) * 8);
 
     auto fetch = [&](const uint8_t *cache, const TileAt<kGroups> &at, uint4 (*to)[kH]) {
 #pragma unroll
@@ -589,8 +646,11 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         walk.template begin<1>(kt0, w.k1, at, [&](int) {
             fetch(a.k_cache, at[0], kb);
             fetch(a.v_cache, at[0], vb);
-        });
+        }, [&] { return come_near(queries); });
     }
+    bf16x8_t qf[2 * kH][kQ];
+#pragma unroll
+    for (int c = 0; c < 2 * kH; ++c) queries[c].planes(qf[c]);
     // (the queries are waited for here, not in the loop)
 #pragma unroll
     for (int c = 0; c < 2 * kH; ++c)
@@ -777,11 +837,13 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     bf16x8_t qf[kFp8 ? 1 : 2 * kC][kQ];
     i32x8_t q8[kFp8 ? kC / 2 : 1][2];
     int q8_scale[2];
+    QueryPiece<T> queries[kFp8 ? 1 : 2 * kC];
+    bool far = false;
     if constexpr (kFp8) {
-        load_query_fp8<kC / 2>(a, row, g, q8, q8_scale);
+        far = load_query_fp8<kC / 2>(a, row, g, q8, q8_scale);
     } else {
 #pragma unroll
-        for (int c = 0; c < 2 * kC; ++c) load_query<T>(a, row, (c >> 1) * 32 + g * 16 + (c & 1) * 8, qf[c]);
+        for (int c = 0; c < 2 * kC; ++c) queries[c].load(a, row, (c >> 1) * 32 + g * 16 + (c & 1) * 8);
     }
 
     struct Values {
@@ -818,6 +880,9 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
         walk.template begin<kStages>(kt0, w.k1, ats, [&](int i) {
             fetch_keys(ats[i], kbs[i]);
             fetch_values(ats[i], vbs[i]);
+        }, [&] {
+            if constexpr (!kFp8) far = come_near(queries);
+            return far;
         });
     }
     // (the queries are waited for here, not in the loop)
@@ -829,6 +894,8 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) asm volatile("" ::"v"(q8[m][q][i]));
     } else {
+#pragma unroll
+        for (int c = 0; c < 2 * kC; ++c) queries[c].planes(qf[c]);
 #pragma unroll
         for (int c = 0; c < 2 * kC; ++c)
 #pragma unroll

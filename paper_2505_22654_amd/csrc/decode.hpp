@@ -81,10 +81,11 @@ struct AttendArgs {
     float *part_acc;               // [B*Hkv, rows, chunks, dp], chunks > 1 only
     float *part_stat;              // [B*Hkv, rows, chunks, 2]: maximum, sum
     int B, Hq, Hkv, T, dh, block_shift, n_blocks, max_blocks, max_len, is_bf16;
-    float scale;                   // times log2(e)
+    float scale, far_scale;        // times log2(e), and that times kFarScale
     int row_tiles, row_waves, row_blocks, chunk, chunks;  // attend_form
 };
 constexpr int kAttendWaves = 4;
+constexpr float kFarScale = 0x1p24f;
 // Keys that a wave takes at a time, by the tiles of 16 rows that it holds.
 constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
 constexpr bool attend_many_fits(bool is_bf16, int head_dim) { return is_bf16 || head_dim <= 192; }

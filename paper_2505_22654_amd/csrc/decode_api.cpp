@@ -268,6 +268,7 @@ int plan_attend(const vscan_cache_desc *d, AttendPlan *p) {
     a.max_len = d->max_len ? d->max_len : d->max_blocks * d->block_size;
     a.is_bf16 = d->dtype == VSCAN_BF16;
     a.scale = (d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim)) * 1.44269504088896341f;
+    a.far_scale = a.scale * kFarScale;
     p->off_stat = p->bytes = 0;
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T;
     // rows, and keys a few tiles past the last one, are counted in 32 bits

@@ -122,3 +122,34 @@ def test_an_infinite_query_is_nan_also_where_every_logit_is_minus_infinity(dtype
     assert torch.equal(got[~odd], want[~odd]) and not want.isnan().any()
     assert bool(got[odd].isnan().all())
     assert not got[1].any() and (present or not got.any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,dh,T", [(4, 2, 64, 1), (8, 1, 256, 1), (4, 2, 128, 3), (4, 2, 128, 40), (2, 1, 192, 70)])
+@pytest.mark.parametrize("length", [33, 1500])
+def test_queries_at_the_top_of_the_range(dtype, hq, hkv, dh, T, length):
+    """Queries of 2^119 to 2^126 and keys of 2^-114: products with the keys as they are stored, up to 448, pass
+    fp32's range, the logits are of order 1 (the scale is 2^-9).  Other rows, and in fp32 entries of the largest
+    fp32 number, which no bf16 number is near: the keys are 2^-129 there."""
+    import torch
+    shape = wl.CacheShape(dtype, 2, hq, hkv, dh, 16, 2 * (-(-length // 16)) + 1, -(-length // 16), T, scale=2.0 ** -9)
+    g = torch.Generator(device="cuda").manual_seed(length + T)
+    dt = vb._torch_dtype(dtype)
+    k = torch.randn((2, hkv, length, dh), generator=g, device="cuda") * 2.0 ** -114
+    q = torch.randn((2, hq, T, dh), generator=g, device="cuda") * 2.0 ** 124
+    q = torch.where(q.abs() < 2.0 ** 119, 2.0 ** 119, q)
+    if dtype == "f32":
+        k[..., 7] = torch.where(k[..., 7] > 0, 2.0 ** -129, -(2.0 ** -129))
+        q[..., 7] = torch.where(q[..., 7] > 0, 1.0, -1.0) * torch.finfo(torch.float32).max
+    q[:, hq - 1] *= 2.0 ** -20                        # rows that would do without
+    v = torch.randn((2, hkv, length, dh), generator=g, device="cuda").to(dt)
+    lens = [length, 17]
+    cache, table, rows = _stored(shape, k.to(dt), v, lens)
+    q = q.to(dt)
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    want, bound = ref.attend(shape, q, rows["k"], rows["v"], cache["v_scale"], table, lens, None)
+    assert bool(torch.isfinite(got).all())
+    over = (got.double() - want).abs() - bound - HALF_STEP[dtype] * want.abs()
+    assert float(over.max()) <= 0, float(over.max())
+    # weights are spread, so that a wrong logit shows
+    assert float((got.double() - want).norm() / want.norm()) < 0.02 and bool(want.any())

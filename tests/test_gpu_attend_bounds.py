@@ -153,3 +153,41 @@ def test_queries_at_the_top_of_the_range(dtype, hq, hkv, dh, T, length):
     assert float(over.max()) <= 0, float(over.max())
     # weights are spread, so that a wrong logit shows
     assert float((got.double() - want).norm() / want.norm()) < 0.02 and bool(want.any())
+
+
+def _many_rows_bound(shape, q, rows, cache, table, lens):
+    """(result, bound) in 64 bits of a bf16 call of more than 16 rows: what fp32 calls are held to, beside it 2^-11
+    of a weight for its one plane of fp16 (or 2^-29 of values of at most 448 scales a key, as above), and twice 2^-14
+    of a weight for logits of base 2 that are off by that at most (ln 2 of it, in the weight and in the sum)."""
+    import dataclasses
+    f32 = dataclasses.replace(shape, dtype="f32")
+    want, bound = ref.attend(f32, q, rows["k"], rows["v"], cache["v_scale"], table, lens, None)
+    size, _ = ref.attend(f32, q, rows["k"], rows["v"].abs(), cache["v_scale"], table, lens, None)
+    return want, bound + (2.0 ** -11 + 2 * 2.0 ** -14) * size + max(lens) * 448 * 2.0 ** -29 * float(cache["v_scale"].max())
+
+
+@pytest.mark.parametrize("B,hq,hkv,dh,T,length", [(2, 4, 2, 128, 40, 90), (2, 8, 1, 64, 30, 1500), (2, 2, 1, 256, 70, 300),
+                                                  (2, 4, 2, 192, 33, 2600), (64, 8, 4, 128, 40, 100), (1, 2, 2, 72, 300, 2400)])
+@pytest.mark.parametrize("apart", [8, 14, 20, 40, 126])
+def test_queries_with_one_entry_far_above_the_others(B, hq, hkv, dh, T, length, apart):
+    """An entry 2^apart of the others', in a dim where the keys are 0 or, in the last fifth of the tokens, whose
+    keys are 2^8 times larger, as small as the format holds: the logits are those of the other entries."""
+    import torch
+    per = -(-length // 16)
+    shape = wl.CacheShape("bf16", B, hq, hkv, dh, 16, B * per + 1, per, T)
+    g = torch.Generator(device="cuda").manual_seed(apart + dh)
+    k = torch.randn((B, hkv, length, dh), generator=g, device="cuda")
+    k[..., 7] = 0
+    last = length * 4 // 5 // 16 * 16
+    k[:, :, last:] *= 2.0 ** 8
+    v = torch.randn((B, hkv, length, dh), generator=g, device="cuda").bfloat16()
+    lens = [length - 3 * (b % 5) for b in range(B)]
+    cache, table, rows = _stored(shape, k.bfloat16(), v, lens)
+    q = torch.randn((B, hq, T, dh), generator=g, device="cuda") * 2.0 ** -6
+    q[..., 7] = 2.0 ** (apart - 6)
+    q[0, 0, 0, 7] = 0
+    q = q.bfloat16()
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    want, bound = _many_rows_bound(shape, q, rows, cache, table, lens)
+    over = (got.double() - want).abs() - bound - HALF_STEP["bf16"] * want.abs()
+    assert float(over.max()) <= 0, float(over.max())

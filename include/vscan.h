@@ -352,8 +352,9 @@ int vscan_encoder_reduce_fused(const vscan_encoder_desc *desc, const void *hidde
  * with p the position of token s of sequence b on axis a(i) (time, height,
  * width, ...).  `inverse` turns by -w, which undoes the rotation and is the
  * gradient of the call with respect to its input.  Entries past rot_dim are
- * copied.  Angles are reduced in 64 bits, so far positions lose nothing; the
- * rotation itself is in 32 bits, rounded once to `dtype`.
+ * copied.  Angles are reduced from the exact product of position and frequency, so
+ * far positions lose nothing (|w| < 2^50); the rotation itself is in 32 bits, rounded
+ * once to `dtype`.
  * ------------------------------------------------------------------------- */
 
 /* a(i): the sections one after the other, or pairs dealt to the axes in turn, an

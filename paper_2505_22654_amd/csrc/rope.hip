@@ -1,7 +1,8 @@
 // Rotary positions of q and k over several axes.
 //
-// A row's pair (x, y) is turned by w = position * frequency.  w is reduced to a quadrant and a rest
-// of at most pi/4 in 64 bits; sine and cosine of the rest are their Taylor sums to x^9 and x^10 in
+// A row's pair (x, y) is turned by w = position * frequency.  The exact product, as two 64-bit numbers, is
+// reduced to a quadrant and a rest of at most pi/4, with pi/2 in two parts (rounded, the product alone would be
+// off by 2^-23 at the ends of 32 bits); sine and cosine of the rest are their Taylor sums to x^9 and x^10 in
 // 32 bits (remainders 1.8e-9 and 1.2e-10 at pi/4).  Angles depend on the token and the pair only, so
 // a thread keeps its pairs' values and walks over heads with them.  Bound: HBM, a read and a write of
 // every entry.  Angles handed around through LDS, with neighbouring heads in one workgroup, took 17.2 to
@@ -16,9 +17,10 @@ namespace {
 using namespace vscan;
 
 __device__ __forceinline__ void turn(int position, double freq, bool inverse, float &c, float &s) {
-    const double quarter = (double)position * freq * 0.63661977236758134308;  // 2 / pi
-    const double n = rint(quarter);
-    const float a = (float)((quarter - n) * 1.57079632679489661923);
+    const double w = (double)position * freq, rest = fma((double)position, freq, -w);
+    const double n = rint(w * 0.63661977236758134308);  // 2 / pi
+    // w - n pi/2: the first part of pi/2 leaves an exact difference, to 2^-53
+    const float a = (float)(fma(-n, 1.57079632679489655800, w) + fma(-n, 6.12323399573676603587e-17, rest));
     const int quadrant = (int)(n - 4.0 * floor(n * 0.25));
     const float z = a * a;
     const float sn = fmaf(a * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), a);

@@ -6,7 +6,7 @@
 // 32 bits (remainders 1.8e-9 and 1.2e-10 at pi/4).  Angles depend on the token and the pair only, so
 // a thread keeps its pairs' values and walks over heads with them.  Bound: HBM, a read and a write of
 // every entry.  Angles handed around through LDS, with neighbouring heads in one workgroup, took 17.2 to
-// 20.5 us where this takes 16.9 (4352 tokens x 32 heads x 128, from the caches, before the hint below).
+// 20.5 us where this takes 16.9 (4352 tokens x 32 heads x 128, from the caches).
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -33,9 +33,17 @@ __device__ __forceinline__ void turn(int position, double freq, bool inverse, fl
     if (inverse) s = -s;
 }
 
-__device__ __forceinline__ void put16(char *p, const uint4 &v, bool stream) {
-    if (stream) store16_stream(p, v);
-    else *reinterpret_cast<uint4 *>(p) = v;
+// As vectors: the compiler takes a struct apart and stores its bytes in pieces of 2, 4 and 8.  Ten sets of inputs in
+// turn, more than the caches hold, us in pieces, whole, and whole with the non-temporal hint:
+//   4352 tokens x 32 heads x 128 in bf16: 23.6, 18.6 (3.8 TB/s; 15.5 on one set, from the caches), 19.5
+//   2 x 4096 tokens x 40 heads x 128 in bf16: 39.5, 31.4 (5.3 TB/s), 35.6; x 72, in pieces of 8 bytes: 33.6, 25.8
+//   2 x 2745 tokens x 32 heads x 80 in fp32: 28.7, 25.4 (4.4 TB/s), 28.7
+__device__ __forceinline__ void put16(char *p, const uint4 &v) {
+    *reinterpret_cast<u32x4_t *>(p) = u32x4_t{v.x, v.y, v.z, v.w};
+}
+__device__ __forceinline__ void put8(char *p, const uint2 &v) {
+    typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<u32x2_t *>(p) = u32x2_t{v.x, v.y};
 }
 // N consecutive entries of a row: 8 or 16 bytes
 template <typename T, int N>
@@ -45,13 +53,13 @@ struct Piece<bf16_t, 8> {
     uint4 raw;
     __device__ __forceinline__ void load(const char *p) { raw = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void get(float *f) const { unpack16<bf16_t>(raw, f); }
-    __device__ __forceinline__ void store(char *p, const float *f, bool stream) const {
+    __device__ __forceinline__ void store(char *p, const float *f) const {
         union {
             __bf16 h[8];
             uint4 u;
         } o;
         for (int i = 0; i < 8; ++i) o.h[i] = (__bf16)f[i];
-        put16(p, o.u, stream);
+        put16(p, o.u);
     }
 };
 template <>
@@ -64,13 +72,13 @@ struct Piece<bf16_t, 4> {
         f[2] = bf16_lo(raw.y);
         f[3] = bf16_hi(raw.y);
     }
-    __device__ __forceinline__ void store(char *p, const float *f, bool) const {
+    __device__ __forceinline__ void store(char *p, const float *f) const {
         union {
             __bf16 h[4];
             uint2 u;
         } o;
         for (int i = 0; i < 4; ++i) o.h[i] = (__bf16)f[i];
-        *reinterpret_cast<uint2 *>(p) = o.u;
+        put8(p, o.u);
     }
 };
 template <>
@@ -78,9 +86,8 @@ struct Piece<float, 4> {
     uint4 raw;
     __device__ __forceinline__ void load(const char *p) { raw = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void get(float *f) const { unpack16<float>(raw, f); }
-    __device__ __forceinline__ void store(char *p, const float *f, bool stream) const {
-        put16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])),
-              stream);
+    __device__ __forceinline__ void store(char *p, const float *f) const {
+        put16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
     }
 };
 
@@ -89,7 +96,7 @@ constexpr int kThreads = 256;
 // N: entries of a piece.  In halves a thread owns a piece of either half (N pairs); with adjacent
 // pairs one piece (N/2 pairs).  Pieces of the entries past rot_dim are copied where a tensor is not
 // turned in place.
-template <typename T, int N, bool ADJ, bool kStream>
+template <typename T, int N, bool ADJ>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, int rest, int per_slice) {
     const int id = blockIdx.x * kThreads + threadIdx.x;
     const int all = pieces + rest;
@@ -124,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, 
         p.load(src);
         if (!turned) {
             p.get(x);
-            p.store(dst, x, kStream);
+            p.store(dst, x);
             continue;
         }
         if constexpr (ADJ) {
@@ -134,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, 
                 y[2 * e] = x[2 * e] * c[e] - x[2 * e + 1] * sn[e];
                 y[2 * e + 1] = x[2 * e] * sn[e] + x[2 * e + 1] * c[e];
             }
-            p.store(dst, y, kStream);
+            p.store(dst, y);
         } else {
             p2.load(src + second);
             p.get(x);
@@ -145,32 +152,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int pieces, 
                 x[e] = u;
                 y[e] = v;
             }
-            p.store(dst, x, kStream);
-            p2.store(dst + second, y, kStream);
+            p.store(dst, x);
+            p2.store(dst + second, y);
         }
     }
 }
 
-// Whether stores carry the non-temporal hint: where more is written than the L2s hold (32 MB) and the
-// pieces of a row fill whole lines of 128 bytes.  Read from memory, without the hint and with it:
-//   4352 tokens x 32 heads x 128 in bf16: 24.0 us, 19.4 (3.7 TB/s; 15.5 us again from the caches)
-//   2 x 4096 tokens x 40 heads x 128 in bf16: 40.6 us, 32.1 (5.2 TB/s, what a copy reaches)
-//   2 x 2745 tokens x 32 heads x 80 in fp32, whose halves share lines: 25.3 us (4.4 TB/s), 29.5
-bool streams(const RopeArgs &a) {
-    const int64_t es = a.is_bf16 ? 2 : 4, run = (a.adjacent ? a.rot : a.rot / 2) * es;
-    if (run % 128 || (int64_t)a.B * a.S * (a.heads[0] + a.heads[1]) * a.rot * es < ((int64_t)32 << 20)) return false;
-    for (int i = 0; i < 2; ++i) {
-        if (!a.heads[i]) continue;
-        if (reinterpret_cast<uintptr_t>(a.out[i]) % 128) return false;
-        for (int64_t stride : a.out_stride[i])
-            if (stride * es % 128) return false;
-    }
-    return true;
-}
-
 // Heads are cut into slices until there are 1024 workgroups: fewer leave loads missing, more work out
-// angles again.  4352 tokens x 32 heads x 128 in bf16, with 256, 512, 1024, 2048 and 4096 workgroups:
-// 32.0, 21.8, 19.4, 19.6, 23.9 us.
+// angles again.  4352 tokens x 32 heads x 128 in bf16, ten sets in turn, with 256, 512, 1024, 2048 and 4096
+// workgroups: 31.2, 21.0, 18.8, 18.9, 22.4 us.
 template <typename T, int N, bool ADJ>
 hipError_t launch(const RopeArgs &a, hipStream_t s) {
     const int pieces = ADJ ? a.rot / N : a.rot / 2 / N;
@@ -182,10 +172,7 @@ hipError_t launch(const RopeArgs &a, hipStream_t s) {
     while (slices < heads && (int64_t)blocks * slices < 1024) slices *= 2;
     const int per = (heads + slices - 1) / slices;
     const dim3 grid(blocks, (heads + per - 1) / per);
-    if (N * sizeof(T) == 16 && streams(a))
-        hipLaunchKernelGGL((rope_kernel<T, N, ADJ, N * sizeof(T) == 16>), grid, dim3(kThreads), 0, s, a, pieces, rest, per);
-    else
-        hipLaunchKernelGGL((rope_kernel<T, N, ADJ, false>), grid, dim3(kThreads), 0, s, a, pieces, rest, per);
+    hipLaunchKernelGGL((rope_kernel<T, N, ADJ>), grid, dim3(kThreads), 0, s, a, pieces, rest, per);
     return hipGetLastError();
 }
 

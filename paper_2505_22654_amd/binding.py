@@ -757,6 +757,7 @@ def cache_store(shape, k, v, slot_map, cache) -> Dict[str, object]:
                and (shape.batch == 1 or k.stride(0) == shape.kv_heads * k.stride(1)),
                f"k, v: expected rows of equal slabs, got strides {k.stride()} and {v.stride()}")
         rows = k.stride(1) // dh
+        _check(rows < 1 << 31, f"k, v: slabs of {rows} rows, which the descriptor does not hold")
     _check_tensor("slot_map", slot_map, torch.int32, (shape.batch, T), index)
     _check_cache(shape, cache, index)
     desc = cache_desc(shape, rows)

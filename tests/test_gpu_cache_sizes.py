@@ -30,3 +30,17 @@ def test_plan_of_the_longest_rows(n_new):
     assert bool((held[:guard] == -7).all()) and bool((held[-guard:] == -7).all())
     for at in range(30, n_new, 1 << 28):
         assert bool((slots[0, at:at + (1 << 28)] == -1).all())
+
+
+def test_store_refuses_slabs_that_a_descriptor_does_not_hold():
+    """2^32 + 50 rows of 8 dims between the heads: cut to 32 bits that would be 50."""
+    import torch
+    rows = (1 << 32) + 50
+    if torch.cuda.mem_get_info()[0] < 2 * (rows * 16 + (1 << 30)):
+        pytest.skip("not enough memory")
+    far = torch.empty(rows * 8 + 64, dtype=torch.bfloat16, device="cuda")   # (never read)
+    x = far.as_strided((1, 2, 3, 8), (2 * rows * 8, rows * 8, 8, 1))
+    shape = wl.CacheShape("bf16", 1, 2, 2, 8, 16, 2, 2, 3)
+    cache = vb.cache_alloc(shape)
+    with pytest.raises(ValueError, match="rows"):
+        vb.cache_store(shape, x, x, i32([[0, 1, 2]]), cache)

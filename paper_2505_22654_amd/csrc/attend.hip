@@ -5,34 +5,36 @@
 // takes them, so they never leave the registers.  The cache is stored in operand order: a lane's 16
 // bytes are one load, and nothing is staged in LDS.
 //
-// bf16 calls: K times q, both exact; V as fp16 (exact) times the weights in fp16: in two planes for up to 16
-// rows, whose sum is a weight to 2^-22 (32 sequences of up to 3427 keys 126.1 us with one, 127.8 with two, bound by
-// memory), in one above, 2^-11 of each weight: a quarter of that is what is left in a sum of many keys, a tenth of
-// the result's own rounding, and the second plane's products would not hide (3 x 300 rows over 2604 keys 42
-// and 54 us, 8 x 512 over 4096 167 and 220).  fp32 calls: q and the weights as three bf16 planes each, V as bf16.  K's scale goes into the logits; V's, a power of two,
-// is taken relative to the largest that the wave has met: down to 2^-15 with the values, beyond that
-// with the weights, whose reference it then enters, so that the largest contributions keep their bits.
+// bf16 calls, up to 16 rows: K times q, both in bf16 as they are; V as fp16 (exact) times the weights in two fp16
+// planes, whose sum is a weight to 2^-22 (32 sequences of up to 3427 keys 126.1 us with one, 127.8 with two, bound by
+// memory).  More rows: q in two e4m3 planes (`query_planes_fp8`), and one plane of weights, 2^-11 of each: a quarter of
+// that is what is left in a sum of many keys, a tenth of the result's own rounding, and the second plane's products
+// would not hide (3 x 300 rows over 2604 keys 42 and 54 us, 8 x 512 over 4096 167 and 220).  fp32 calls: q and the
+// weights as three bf16 planes each, V as bf16.  K's scale goes into the logits; V's, a power of two, is taken
+// relative to the largest that the wave has met: down to 2^-15 with the values, beyond that with the weights, whose
+// reference it then enters, so that the largest contributions keep their bits.
 // Softmax in one pass against a reference that is raised only where a lane's weights of a tile add up to more
 // than 2^12, so that most tiles need no exchange between lanes and no maximum.
 //
 // Two forms, by rows (`attend_form`): up to 16, with 16x16x32 instructions and 64 keys at a time (bound by HBM: 2 dh
-// bytes per token and kv head); more, 32 to a wave, with 32 keys at a time, two tiles in flight.  There a bf16
-// q goes into two e4m3 planes, which are multiplied with K as it is stored, 64 dims an instruction, and V is
-// converted for 32x32x16 instructions (bound by the vector unit beside the matrix pipe: per logit a multiply-add,
-// an exponential and a sum, and V's and the weights' conversions; a matrix instruction keeps the vector unit
-// from issuing for some cycles whatever its size, so the large ones overlap better: 96 multiply-adds and 16
-// exponentials with 514 cycles of them 667, with 16x16x32 861).
+// bytes per token and kv head); more, 32 to a wave, with 32 keys at a time, two tiles in flight.  There the planes
+// of q are multiplied with K as it is stored, 64 dims an instruction, and V is converted for 32x32x16 instructions
+// (bound by the vector unit beside the matrix pipe: per logit a multiply-add, an exponential and a sum, and V's and
+// the weights' conversions; a matrix instruction keeps the vector unit from issuing for some cycles whatever its
+// size, so the large ones overlap better: 96 multiply-adds and 16 exponentials with 514 cycles of them 667, with
+// 16x16x32 861).
 // The four waves of a workgroup take the tiles of its keys in turn and add their results in LDS; where
 // sequences and rows leave compute units idle the keys are cut into chunks over workgroups, which a
 // second launch joins.
 //
-// Measured, bf16, dh = 128, GPU time: one token of 32 sequences with 32 heads, up to 3427 keys, 126 us
-// (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 43 us (50 cold); of one with
-// 2304 keys 9.9 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096 keys 165 us
-// (820 TFLOP/s of the two products), over 8192 300 us (915); 4 x 700 over 3000, 32 heads, 111 us (655); 3 x 300
-// over 2604, 28 of 4, 42 us (460: 396 workgroups on 256 CUs).  With K converted to bf16 and a maximum of each
-// tile these four took 177, 328, 117 and 44.  More rows a wave (64: 280 us where 32 took 179), eight waves (245)
-// and rows over all four waves (203) lost to this split.
+// Measured, bf16, dh = 128, GPU time of calls on one set of inputs: one token of 32 sequences with 32 heads, up to
+// 3427 keys, 127 us (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 44 us (53 on five sets
+// in turn); of one with 2304 keys 10.2 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096
+// keys 171 us (792 TFLOP/s of the two products; 164 to 178 on different cards), over 8192 314 us (875), over 16384
+// 605 us (914); 4 x 700 over 3000, 32 heads, 117 us (623); 3 x 300 over 2604, 28 of 4, 43 us (446: 396 workgroups on
+// 256 CUs).  Two planes and no maximum of a tile, against K in bf16 and one, in turn on one card: 165 and 177 us for
+// the first of these prompts, 300 and 328 for the second.  More rows a wave (64: 280 us where 32 took 179), eight
+// waves (245) and rows over all four waves (203) lost to this split.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>

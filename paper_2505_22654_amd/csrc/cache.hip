@@ -114,7 +114,8 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(PlanArgs a,
 // rounding it holds 32 bytes that belong to pieces of its neighbours: one exchange (k) or a 4x4
 // transposition (v) between lanes of a quad leaves two whole 16-byte pieces of the page per unit.
 // Bound: HBM (2 or 4 bytes in and one out per value).  32 sequences of up to 1267 tokens, 32 heads x 128 in
-// bf16 (803 MB): 154 us cold (5.2 TB/s, as a copy); one token of each 4.7 us, a launch's latency.  With every
+// bf16 (803 MB): 154 us cold (5.2 TB/s, as a copy), in fp32 (1.34 GB) 259; one token of each 4.7 us, in fp32 4.5, a
+// launch's latency.  With every
 // page's rows requested before its slot is known, which hides a load but reads the rows of ragged batches
 // that go nowhere, 190 us; loads with the non-temporal hint 160 (8 heads, 35 MB, from the caches: 31 us
 // without, 36 with); stores with it 258, as no store fills a line by itself.

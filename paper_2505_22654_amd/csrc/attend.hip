@@ -5,24 +5,25 @@
 // takes them, so they never leave the registers.  The cache is stored in operand order: a lane's 16
 // bytes are one load, and nothing is staged in LDS.
 //
-// bf16 calls, up to 16 rows: K times q, both in bf16 as they are; V as fp16 (exact) times the weights in two fp16
-// planes, whose sum is a weight to 2^-22 (32 sequences of up to 3427 keys 126.1 us with one, 127.8 with two, bound by
-// memory).  More rows: q in two e4m3 planes (`query_planes_fp8`), and one plane of weights, 2^-11 of each: a quarter of
-// that is what is left in a sum of many keys, a tenth of the result's own rounding, and the second plane's products
-// would not hide (3 x 300 rows over 2604 keys 42 and 54 us, 8 x 512 over 4096 167 and 220).  fp32 calls: q and the
-// weights as three bf16 planes each, V as bf16.  K's scale goes into the logits; V's, a power of two, is taken
+// bf16 calls: K (as bf16, exact) times q; V as fp16 (exact) times the weights in fp16: in two planes for up to 16
+// rows, whose sum is a weight to 2^-22 (32 sequences of up to 3427 keys 126.1 us with one, 127.8 with two, bound by
+// memory), in one above, 2^-11 of each: a quarter of that is what is left in a sum of many keys, a tenth of the
+// result's own rounding, and the second plane's products would not hide (3 x 300 rows over 2604 keys 42 and 54 us,
+// 8 x 512 over 4096 167 and 220).  fp32 calls: q and the weights as three bf16 planes each, V as bf16.  (The 8-bit
+// instructions would take K as it is stored, with q in two planes, in 165 us where this takes 173.  But they drop what
+// lies 2^-11 to 2^-14 below the largest product of a sum, where those of bf16 keep 2^-21: logits with one large
+// product were off by 1e-2.)  K's scale goes into the logits; V's, a power of two, is taken
 // relative to the largest that the wave has met: down to 2^-15 with the values, beyond that with the weights, whose
 // reference it then enters, so that the largest contributions keep their bits.
 // Softmax in one pass against a reference that is raised only where a lane's weights of a tile add up to more
 // than 2^12, so that most tiles need no exchange between lanes and no maximum.
 //
 // Two forms, by rows (`attend_form`): up to 16, with 16x16x32 instructions and 64 keys at a time (bound by HBM: 2 dh
-// bytes per token and kv head); more, 32 to a wave, with 32 keys at a time, two tiles in flight.  There the planes
-// of q are multiplied with K as it is stored, 64 dims an instruction, and V is converted for 32x32x16 instructions
-// (bound by the vector unit beside the matrix pipe: per logit a multiply-add, an exponential and a sum, and V's and
-// the weights' conversions; a matrix instruction keeps the vector unit from issuing for some cycles whatever its
-// size, so the large ones overlap better: 96 multiply-adds and 16 exponentials with 514 cycles of them 667, with
-// 16x16x32 861).
+// bytes per token and kv head); more, 32 to a wave, with 32x32x16 instructions and 32 keys at a time, two tiles in
+// flight (bound by the vector unit beside the matrix pipe: per logit a multiply-add, an exponential and a sum, and
+// K's, V's and the weights' conversions; a matrix instruction keeps the vector unit from issuing for some cycles
+// whatever its size, so the large ones overlap better: 96 multiply-adds and 16 exponentials with 514 cycles of them
+// 667, with 16x16x32 861).
 // The four waves of a workgroup take the tiles of its keys in turn and add their results in LDS; where
 // sequences and rows leave compute units idle the keys are cut into chunks over workgroups, which a
 // second launch joins.
@@ -214,9 +215,6 @@ __device__ __forceinline__ Row row_of(const AttendArgs &a, const Work &w, int r)
 // Queries at the top of the range.  K goes into the products without its scale, so up to 256 products of 448 and an
 // entry of kFar stay inside fp32; where an entry of a wave's rows is larger, they are all taken by 2^-24, which
 // the factor of the logits makes up for (c above 2^127 then: infinite logits, and NaN).
-// (what all lanes agree on is kept in a scalar register)
-__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
-__device__ __forceinline__ bool uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 constexpr float kFar = 0x1p104f, kNear = 1.f / kFarScale;
 // Eight entries of a query.
 template <typename T>
@@ -285,73 +283,12 @@ __device__ __forceinline__ bool come_near(QueryPiece<T> (&q)[kN]) {
     float top = 0.f;
 #pragma unroll
     for (int c = 0; c < kN; ++c) top = fmaxf(top, q[c].largest());
-    const bool far = uniform(__any(top >= kFar && top < INFINITY));
+    const bool far = __builtin_amdgcn_readfirstlane(__any(top >= kFar && top < INFINITY));
     if (__builtin_expect(far, 0)) {
 #pragma unroll
         for (int c = 0; c < kN; ++c) q[c].come_near();
     }
     return far;
-}
-
-// A bf16 query in two e4m3 planes, for products with K as it is stored: 2^e of a row puts its largest entry
-// at 2^7 to 2^8, hi = q / 2^e rounded to 4 bits, lo = 16 (q / 2^e - hi).  bf16's 8 bits leave lo at most 4, so
-// both are exact for entries down to 2^-13 of the largest (lo's last place is 2^-13), and below it off by 2^-14 of
-// 2^e, 2^-21 of the largest.  What that can move a logit by is known from the row's entries and a block's scale;
-// where it is too much, as with one entry far above the others, K is multiplied in bf16 with q as it is.  The
-// planes' 2^e and 2^(e - 4) are operands of the instruction (exponent bytes).
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
-typedef short i16x2_t __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ i32x8_t eight(const uint4 &a, const uint4 &b) {
-    return i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
-}
-constexpr float kLogitError = 0x1p-14f;  // of a logit of base 2: 2^-14.5 of a weight, whose rounding is 2^-11
-struct Planes {
-    bool far;     // scaled by kNear, which their exponents hold
-    float error;  // at most, of a row's products with keys of 1
-};
-// Row of a lane for products of 64 dims, 32 in each half of the wave: those that its 16-byte pieces of K are.
-template <int kN>
-__device__ __forceinline__ Planes query_planes_fp8(const QueryPiece<bf16_t> (&raw)[4 * kN], i32x8_t (*out)[2], int *scale) {
-    float top = 0.f, error = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4 * kN; ++i) top = fmaxf(top, raw[i].largest());
-    top = fmaxf(top, __shfl_xor(top, 32, kWave));
-    // 2^e with 128 <= top / 2^e < 256
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -96), 120);
-    const bool far = uniform(__any(top >= kFar && top < INFINITY));
-    const int unit = e + 127 - (far ? 24 : 0);
-    scale[0] = top < INFINITY ? unit : 255;  // (255: NaN, where the conversions would end at the largest number)
-    scale[1] = unit - 4;
-    const float hi_unit = pow2(e), lo_unit = pow2(e - 4);
-#pragma unroll
-    for (int m = 0; m < kN; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float f[8];
-            raw[4 * m + i].get(f);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float *x = f + 4 * h;
-                i16x2_t w = {0, 0}, v = {0, 0};
-                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[0], x[1], hi_unit, false);
-                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[2], x[3], hi_unit, true);
-                const int hi = __builtin_bit_cast(int, w);
-                const f32x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, hi_unit, false);
-                const f32x2_t up = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, hi_unit, true);
-                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, x[0] - lo[0], x[1] - lo[1], lo_unit, false);
-                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, x[2] - up[0], x[3] - up[1], lo_unit, true);
-                out[m][0][2 * i + h] = hi;
-                out[m][1][2 * i + h] = __builtin_bit_cast(int, v);
-                const f32x2_t r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(out[m][1][2 * i + h], lo_unit, false);
-                const f32x2_t s = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(out[m][1][2 * i + h], lo_unit, true);
-                error += fabsf(x[0] - lo[0] - r[0]);
-                error += fabsf(x[1] - lo[1] - r[1]);
-                error += fabsf(x[2] - up[0] - s[0]);
-                error += fabsf(x[3] - up[1] - s[1]);
-            }
-        }
-    error = top < INFINITY ? fmaxf(error, 0.f) : 0.f;  // (a row that is not finite is NaN anyway)
-    return {far, uniform(2.f * wave_max(error) * (far ? kNear : 1.f))};
 }
 
 // The keys of a tile: where its groups of 16 lie, and their scales.
@@ -368,21 +305,14 @@ struct TileAt {
 template <int kGroups, int DP>
 struct Walk {
     static constexpr int kBatch = kWave / kGroups;  // tiles
-    static constexpr int kTooCoarse = -1;           // whole_end where planes of the queries are too coarse
     const AttendArgs &a;
     const int32_t *table;
-    int hk, step, k1, batch_kt, located, block_ahead, lane_block, lane_e;
-    int whole_end, end;      // as far as tiles without masks may go, and all
+    int hk, step, k1, batch_kt, located = 0, block_ahead, lane_block, lane_e;
     float lane_c;
-    bool far = false;        // queries are scaled by kNear
-    float error = 0.f;       // what planes of e4m3 leave out of a query, times keys of 1
+    bool far = false;  // queries are scaled by kNear
 
     __device__ __forceinline__ Walk(const AttendArgs &args, int b, int hk_, int step_, int kt)
-        : a(args), table(args.block_table + (int64_t)b * args.max_blocks), hk(hk_), step(step_) {
-        start(kt);
-    }
-    __device__ __forceinline__ void start(int kt) {
-        batch_kt = kt;
+        : a(args), table(args.block_table + (int64_t)b * args.max_blocks), hk(hk_), step(step_), batch_kt(kt) {
         block_ahead = blocks_from();  // ahead of knowing whether the tokens are there
     }
     __device__ __forceinline__ int64_t lane_key() const {
@@ -405,10 +335,6 @@ struct Walk {
     // (waited for at once, so that no later load of the loop is)
     __device__ __forceinline__ void settle() {
         lane_c *= far ? a.far_scale : a.scale;
-        if (uniform(__any(lane_block >= 0 && 448.f * error * lane_c > kLogitError))) {
-            whole_end = kTooCoarse;
-            if constexpr (DP > 128) end = 0;
-        }
         lane_e = lane_block >= 0 ? exp_of(__int_as_float(lane_e)) : kScaleExpMin;
         asm volatile("" ::"v"(block_ahead));
     }
@@ -446,19 +372,18 @@ struct Walk {
             at.e[u] = __builtin_amdgcn_readlane(lane_e, tile * kGroups + u);
         }
     }
-    // The first kStages tiles: their keys and values are requested before their scales have come, and before
-    // `queries` waits for the queries.
-    template <int kStages, typename Fetch, typename Queries>
-    __device__ __forceinline__ void begin(int kt, int last, int whole, TileAt<kGroups> *ats, Fetch fetch, Queries queries) {
-        k1 = end = last;
-        whole_end = whole;
+    // The first kStages tiles: their keys and values are requested before their scales, and what `far` looks
+    // at, the queries, have come.
+    template <int kStages, typename Fetch, typename Far>
+    __device__ __forceinline__ void begin(int kt, int end, TileAt<kGroups> *ats, Fetch fetch, Far is_far) {
+        k1 = end;
         next_batch();
 #pragma unroll
         for (int i = 0; i < kStages; ++i) {
             locate(kt + i * step, ats[i]);
             fetch(i);
         }
-        queries();
+        far = is_far();
         settle();
 #pragma unroll
         for (int i = 0; i < kStages; ++i) scales_of(i, ats[i]);
@@ -486,11 +411,11 @@ struct Scales {
 };
 
 // Walks over the wave's tiles: whole ones, which every row sees and whose blocks are all there, without
-// masks, as far as they come first; then the others.  Ends where the walk does (Walk::end).
-template <int kTile, int kStages, bool kWhole, typename Walk, typename At, typename Tile>
-__device__ __forceinline__ void walk_tiles(int kt, int step, const Walk &walk, const At *ats, Tile tile) {
+// masks, as far as they come first; then the others.
+template <int kTile, int kStages, typename At, typename Tile>
+__device__ __forceinline__ void walk_tiles(int kt, int step, const Work &w, const At *ats, Tile tile) {
     constexpr int kGroups = kTile / kCacheGroup;
-    while (kWhole && kt + (kStages - 1) * step + kTile <= walk.whole_end) {
+    while (kt + (kStages - 1) * step + kTile <= min(w.k1, w.all_see)) {
         bool whole = true;
 #pragma unroll
         for (int i = 0; i < kStages; ++i)
@@ -500,10 +425,10 @@ __device__ __forceinline__ void walk_tiles(int kt, int step, const Walk &walk, c
 #pragma unroll
         for (int i = 0; i < kStages; ++i, kt += step) tile(std::false_type(), i, kt);
     }
-    while (kt < walk.end) {
+    while (kt < w.k1) {
 #pragma unroll
         for (int i = 0; i < kStages; ++i)
-            if (kt < walk.end) {
+            if (kt < w.k1) {
                 tile(std::true_type(), i, kt);
                 kt += step;
             }
@@ -656,10 +581,10 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     TileAt<kGroups> at[1];
     uint4 kb[kGroups][kH], vb[kGroups][kH];
     if (kt0 < w.k1) {
-        walk.template begin<1>(kt0, w.k1, min(w.k1, w.all_see), at, [&](int) {
+        walk.template begin<1>(kt0, w.k1, at, [&](int) {
             fetch(a.k_cache, at[0], kb);
             fetch(a.v_cache, at[0], vb);
-        }, [&] { walk.far = come_near(queries); });
+        }, [&] { return come_near(queries); });
     }
     bf16x8_t qf[2 * kH][kQ];
 #pragma unroll
@@ -677,7 +602,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 #pragma unroll
     for (int d = 0; d < kD; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    if (kt0 < w.k1) walk_tiles<kTile, 1, true>(kt0, step, walk, at, [&](auto masked, int, int kt) {
+    walk_tiles<kTile, 1>(kt0, step, w, at, [&](auto masked, int, int kt) {
         constexpr bool kMask = decltype(masked)::value;
         TileAt<kGroups> next;
         walk.locate(kt + step, next);
@@ -846,16 +771,9 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     if (a.chunks > 1 && w.k0 >= w.block_reach) return;
 
     const Row row = row_of(a, w, w.row0 + j);
-    constexpr bool kFp8 = sizeof(T) == 2;
-    bf16x8_t qf[kFp8 ? 1 : 2 * kC][kQ];
-    i32x8_t q8[kFp8 ? kC / 2 : 1][2];
-    int q8_scale[2];
     QueryPiece<T> queries[2 * kC];
 #pragma unroll
     for (int c = 0; c < 2 * kC; ++c) queries[c].load(a, row, (c >> 1) * 32 + g * 16 + (c & 1) * 8);
-    // where the rows are, for products with them as they are (in what holds the statistics in the end)
-    int64_t *const rows_at = reinterpret_cast<int64_t *>(lds4 + kWaves * (kD / 2) * 4 * kWave) + wave * 32;
-    if (kFp8 && g == 0) rows_at[j] = row.padding ? -1 : row.at;
 
     struct Values {
         uint4 pair[4][kPairs > 0 ? kPairs : 1];  // [tokens 8a + 4g ..][pair of 64 dims]
@@ -887,191 +805,132 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     TileAt<kGroups> ats[kStages];
     uint4 kbs[kStages][kC];
     Values vbs[kStages];
+    if (kt0 < w.k1) {
+        walk.template begin<kStages>(kt0, w.k1, ats, [&](int i) {
+            fetch_keys(ats[i], kbs[i]);
+            fetch_values(ats[i], vbs[i]);
+        }, [&] { return come_near(queries); });
+    }
+    bf16x8_t qf[2 * kC][kQ];
+#pragma unroll
+    for (int c = 0; c < 2 * kC; ++c) queries[c].planes(qf[c]);
+    // (the queries are waited for here, not in the loop)
+#pragma unroll
+    for (int c = 0; c < 2 * kC; ++c)
+#pragma unroll
+        for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[c][q]));
+
     f32x16_t acc[kD];
-    float m, l;
-    int eref, nan_from;
-    // Over the wave's tiles.  Where planes of q are too coarse, the masked tiles take q as it is, or with heads above 128,
-    // whose registers that would not fit beside, all tiles are done again by a run of its own (kExact; 8 x 512 rows
-    // over 4096 keys, heads of 256: 403 us, in the masked tiles 440).  Nothing that only this takes is kept in registers.
-    auto run = [&](auto exact) __attribute__((always_inline)) {
-        constexpr bool kExact = decltype(exact)::value;
-        if (kt0 < w.k1) {
-            walk.template begin<kStages>(kt0, w.k1, min(w.k1, w.all_see), ats, [&](int i) {
-                fetch_keys(ats[i], kbs[i]);
-                fetch_values(ats[i], vbs[i]);
-            }, [&] {
-                if constexpr (kExact) {
-                    walk.error = 0.f;
-                } else if constexpr (kFp8) {
-                    const Planes p = query_planes_fp8<kC / 2>(queries, q8, q8_scale);
-                    walk.far = p.far;
-                    walk.error = p.error;
-                } else {
-                    walk.far = come_near(queries);
-                }
-            });
-        }
-        // (the queries are waited for here, not in the loop)
-        if constexpr (kFp8 && !kExact) {
+    float m = kNothing, l = 0.f;
+    int eref = kScaleExpMin, nan_from = INT_MAX;
 #pragma unroll
-            for (int m = 0; m < kC / 2; ++m)
+    for (int d = 0; d < kD; ++d)
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) asm volatile("" ::"v"(q8[m][q][i]));
-        } else if constexpr (!kExact) {
-#pragma unroll
-            for (int c = 0; c < 2 * kC; ++c) queries[c].planes(qf[c]);
-#pragma unroll
-            for (int c = 0; c < 2 * kC; ++c)
-#pragma unroll
-                for (int q = 0; q < kQ; ++q) asm volatile("" ::"v"(qf[c][q]));
-        }
-        m = kNothing;
-        l = 0.f;
-        eref = kScaleExpMin;
-        nan_from = INT_MAX;
-#pragma unroll
-        for (int d = 0; d < kD; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
 
-        if (kt0 < w.k1) walk_tiles<kTile, kStages, !kExact>(kt0, step, walk, ats, [&](auto masked, int stage, int kt) {
-            constexpr bool kMask = decltype(masked)::value;
-            TileAt<kGroups> &at = ats[stage], next;
-            uint4 *kb = kbs[stage];
-            Values &vb = vbs[stage];
-            walk.locate(kt + kStages * step, next);
-            f32x16_t s;
+    walk_tiles<kTile, kStages>(kt0, step, w, ats, [&](auto masked, int stage, int kt) {
+        constexpr bool kMask = decltype(masked)::value;
+        TileAt<kGroups> &at = ats[stage], next;
+        uint4 *kb = kbs[stage];
+        Values &vb = vbs[stage];
+        walk.locate(kt + kStages * step, next);
+        f32x16_t s;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = 0.f;
-            if (kExact || (kFp8 && kMask && DP <= 128 && __builtin_expect(walk.whole_end == walk.kTooCoarse, 0))) {
-                unsigned none = 0;
-                asm volatile("" : "+s"(none));
-                const int here = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
-                Row again;
-                again.at = rows_at[here & 31];
-                again.padding = false;
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-                for (int c = 0; c < 2 * kC; ++c) {
-                    QueryPiece<T> q;
-                    bf16x8_t v[kQ];
-                    q.load(a, again, (c >> 1) * 32 + (here >> 5) * 16 + (c & 1) * 8);
-                    if (walk.far) q.come_near();
-                    q.planes(v);
-                    const bf16x8_t ka = from_fp8<Operand<float>>(word(kb[c >> 1], 2 * (c & 1)), word(kb[c >> 1], 2 * (c & 1) + 1), 1.f, 1.f);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, v[0], s, 0, 0, 0);
-                }
-            } else if constexpr (kFp8) {
+        for (int c = 0; c < 2 * kC; ++c) {
+            const bf16x8_t ka = from_fp8<Operand<float>>(word(kb[c >> 1], 2 * (c & 1)), word(kb[c >> 1], 2 * (c & 1) + 1), 1.f, 1.f);
 #pragma unroll
-                for (int m = 0; m < kC / 2; ++m)
-#pragma unroll
-                    for (int q = 1; q >= 0; --q)
-                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(eight(kb[2 * m], kb[2 * m + 1]), q8[m][q], s, 0, 0, 0, 127, 0, q8_scale[q]);
-            } else {
-#pragma unroll
-                for (int c = 0; c < 2 * kC; ++c) {
-                    const bf16x8_t ka = from_fp8<Operand<float>>(word(kb[c >> 1], 2 * (c & 1)), word(kb[c >> 1], 2 * (c & 1) + 1), 1.f, 1.f);
-#pragma unroll
-                    for (int q = kQ - 1; q >= 0; --q) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[c][q], s, 0, 0, 0);
-                }
-            }
-            fetch_keys(next, kb);
+            for (int q = kQ - 1; q >= 0; --q) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[c][q], s, 0, 0, 0);
+        }
+        fetch_keys(next, kb);
 
-            Scales<kGroups, sizeof(T) == 2> sc;
-            sc.of(at, eref);
-            __builtin_amdgcn_sched_barrier(0);
-            typename O::vec pb[kGroups][kP];
-            float sums[kGroups];
-            auto logit = [&](int r, float add) {
-                float v = fmaf(s[r], at.c[r >> 3], add);
-                if constexpr (kMask) v = at.there[r >> 3] && kt + 8 * (r >> 2) + 4 * g + (r & 3) < row.lim ? v : -INFINITY;
-                return v;
-            };
-            auto weigh = [&](float ref) {
-#pragma unroll
-                for (int u = 0; u < kGroups; ++u) {
-                    const float add = sc.weights[u] - ref;
-                    sums[u] = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 8; r += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(logit(8 * u + r, add)), p1 = __builtin_amdgcn_exp2f(logit(8 * u + r + 1, add));
-                        typename O::pair pp[kP];
-                        split<O, kP>(f32x2_t{p0, p1}, pp);
-                        sums[u] += p0;
-                        sums[u] += p1;
-#pragma unroll
-                        for (int q = 0; q < kP; ++q) {
-                            pb[u][q][r] = pp[q][0];
-                            pb[u][q][r + 1] = pp[q][1];
-                        }
-                    }
-                }
-                return sums[0] + sums[1];
-            };
-            if (__any(weigh(m) > kRaise) || sc.now > eref) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, logit(r, sc.weights[r >> 3]));
-                top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
-                m = now;
-                eref = __builtin_amdgcn_readfirstlane(sc.now);
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < kD; ++d) acc[d] *= fu;
-                weigh(now);
-            }
-            if constexpr (kMask) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t keep = value_mask(w.sp.len - (kt + 8 * q + 4 * g), at.there[q >> 1]);
-#pragma unroll
-                    for (int p = 0; p < kPairs; ++p) {
-                        vb.pair[q][p].x &= keep;
-                        vb.pair[q][p].y &= keep;
-                        vb.pair[q][p].z &= keep;
-                        vb.pair[q][p].w &= keep;
-                    }
-                    if constexpr (kOdd) {
-                        vb.odd[q].x &= keep;
-                        vb.odd[q].y &= keep;
-                    }
-                }
-                uint32_t nan = 0;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-#pragma unroll
-                    for (int p = 0; p < kPairs; ++p)
-                        nan |= take_nan(vb.pair[q][p].x) | take_nan(vb.pair[q][p].y) | take_nan(vb.pair[q][p].z) | take_nan(vb.pair[q][p].w);
-                    if constexpr (kOdd) nan |= take_nan(vb.odd[q].x) | take_nan(vb.odd[q].y);
-                }
-                if (__any(nan)) nan_from = min(nan_from, kt);
-            }
+        Scales<kGroups, sizeof(T) == 2> sc;
+        sc.of(at, eref);
+        __builtin_amdgcn_sched_barrier(0);
+        typename O::vec pb[kGroups][kP];
+        float sums[kGroups];
+        auto logit = [&](int r, float add) {
+            float v = fmaf(s[r], at.c[r >> 3], add);
+            if constexpr (kMask) v = at.there[r >> 3] && kt + 8 * (r >> 2) + 4 * g + (r & 3) < row.lim ? v : -INFINITY;
+            return v;
+        };
+        auto weigh = [&](float ref) {
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
-                l = fmaf(sums[u], sc.sums[u], l);
+                const float add = sc.weights[u] - ref;
+                sums[u] = 0.f;
 #pragma unroll
-                for (int d = 0; d < kD; ++d) {
-                    uint32_t lo, up;
-                    value_words(vb, u, d, lo, up);
-                    const typename O::vec vv = from_fp8<O>(lo, up, sc.values[u], sc.values[u]);
+                for (int r = 0; r < 8; r += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(logit(8 * u + r, add)), p1 = __builtin_amdgcn_exp2f(logit(8 * u + r + 1, add));
+                    typename O::pair pp[kP];
+                    split<O, kP>(f32x2_t{p0, p1}, pp);
+                    sums[u] += p0;
+                    sums[u] += p1;
 #pragma unroll
-                    for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma32(vv, pb[u][q], acc[d]);
+                    for (int q = 0; q < kP; ++q) {
+                        pb[u][q][r] = pp[q][0];
+                        pb[u][q][r + 1] = pp[q][1];
+                    }
                 }
             }
-            fetch_values(next, vb);
-            at = next;
-            if constexpr (sizeof(T) == 4 || DP > 128) settle_products<4>();
-        });
-    };
-    run(std::false_type());
-    if constexpr (kFp8 && DP > 128) {
-        if (__builtin_expect(kt0 < w.k1 && walk.end == 0, 0)) {
-            walk.start(kt0);
-            run(std::true_type());
+            return sums[0] + sums[1];
+        };
+        if (__any(weigh(m) > kRaise) || sc.now > eref) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, logit(r, sc.weights[r >> 3]));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
+            m = now;
+            eref = __builtin_amdgcn_readfirstlane(sc.now);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < kD; ++d) acc[d] *= fu;
+            weigh(now);
         }
-    }
+        if constexpr (kMask) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t keep = value_mask(w.sp.len - (kt + 8 * q + 4 * g), at.there[q >> 1]);
+#pragma unroll
+                for (int p = 0; p < kPairs; ++p) {
+                    vb.pair[q][p].x &= keep;
+                    vb.pair[q][p].y &= keep;
+                    vb.pair[q][p].z &= keep;
+                    vb.pair[q][p].w &= keep;
+                }
+                if constexpr (kOdd) {
+                    vb.odd[q].x &= keep;
+                    vb.odd[q].y &= keep;
+                }
+            }
+            uint32_t nan = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int p = 0; p < kPairs; ++p)
+                    nan |= take_nan(vb.pair[q][p].x) | take_nan(vb.pair[q][p].y) | take_nan(vb.pair[q][p].z) | take_nan(vb.pair[q][p].w);
+                if constexpr (kOdd) nan |= take_nan(vb.odd[q].x) | take_nan(vb.odd[q].y);
+            }
+            if (__any(nan)) nan_from = min(nan_from, kt);
+        }
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            l = fmaf(sums[u], sc.sums[u], l);
+#pragma unroll
+            for (int d = 0; d < kD; ++d) {
+                uint32_t lo, up;
+                value_words(vb, u, d, lo, up);
+                const typename O::vec vv = from_fp8<O>(lo, up, sc.values[u], sc.values[u]);
+#pragma unroll
+                for (int q = kP - 1; q >= 0; --q) acc[d] = O::mfma32(vv, pb[u][q], acc[d]);
+            }
+        }
+        fetch_values(next, vb);
+        at = next;
+        if constexpr (sizeof(T) == 4 || DP > 128) settle_products<4>();
+    });
 
     settle_products<4>();
     if (nan_from < w.k1) {

@@ -156,14 +156,13 @@ def test_queries_at_the_top_of_the_range(dtype, hq, hkv, dh, T, length):
 
 
 def _many_rows_bound(shape, q, rows, cache, table, lens):
-    """(result, bound) in 64 bits of a bf16 call of more than 16 rows: what fp32 calls are held to, beside it 2^-11
-    of a weight for its one plane of fp16 (or 2^-29 of values of at most 448 scales a key, as above), and twice 2^-14
-    of a weight for logits of base 2 that are off by that at most (ln 2 of it, in the weight and in the sum)."""
+    """(result, bound) in 64 bits of a bf16 call of more than 16 rows: what fp32 calls are held to, and 2^-11 of a
+    weight for its one plane of fp16 (or 2^-29 of values of at most 448 scales a key, as above)."""
     import dataclasses
     f32 = dataclasses.replace(shape, dtype="f32")
     want, bound = ref.attend(f32, q, rows["k"], rows["v"], cache["v_scale"], table, lens, None)
     size, _ = ref.attend(f32, q, rows["k"], rows["v"].abs(), cache["v_scale"], table, lens, None)
-    return want, bound + (2.0 ** -11 + 2 * 2.0 ** -14) * size + max(lens) * 448 * 2.0 ** -29 * float(cache["v_scale"].max())
+    return want, bound + 2.0 ** -11 * size + max(lens) * 448 * 2.0 ** -29 * float(cache["v_scale"].max())
 
 
 @pytest.mark.parametrize("B,hq,hkv,dh,T,length", [(2, 4, 2, 128, 40, 90), (2, 8, 1, 64, 30, 1500), (2, 2, 1, 256, 70, 300),
@@ -191,3 +190,26 @@ def test_queries_with_one_entry_far_above_the_others(B, hq, hkv, dh, T, length, 
     want, bound = _many_rows_bound(shape, q, rows, cache, table, lens)
     over = (got.double() - want).abs() - bound - HALF_STEP["bf16"] * want.abs()
     assert float(over.max()) <= 0, float(over.max())
+
+
+@pytest.mark.parametrize("hq,hkv,dh,T,length", [(16, 4, 24, 40, 400), (2, 2, 16, 257, 300), (8, 1, 192, 9, 1500), (4, 1, 128, 16, 60),
+                                                (6, 2, 80, 33, 700), (2, 1, 256, 64, 200), (4, 4, 64, 33, 2000)])
+@pytest.mark.parametrize("gain", [16.0, 64.0])
+def test_logits_with_a_large_product_keep_the_small_ones(hq, hkv, dh, T, length, gain):
+    """One dim of the queries `gain` times the others, as models have them: logits of up to some hundred, whose
+    differences are held to fp32 sums, (dh + 8) 2^-24 of the products' sizes, whatever the largest is."""
+    import torch
+    per = -(-length // 16)
+    shape = wl.CacheShape("bf16", 2, hq, hkv, dh, 16, 2 * per + 1, per, T)
+    g = torch.Generator(device="cuda").manual_seed(dh + T)
+    k = torch.randn((2, hkv, length, dh), generator=g, device="cuda").bfloat16()
+    v = torch.randn((2, hkv, length, dh), generator=g, device="cuda").bfloat16()
+    lens = [length, length - 7]
+    cache, table, rows = _stored(shape, k, v, lens)
+    q = torch.randn((2, hq, T, dh), generator=g, device="cuda") * 2
+    q[..., 3] *= gain
+    q = q.bfloat16()
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"]
+    want, bound = _many_rows_bound(shape, q, rows, cache, table, lens)
+    over = (got.double() - want).abs() - bound - HALF_STEP["bf16"] * want.abs()
+    assert float(over.max()) <= 0, (float(over.max()), int((over > 0).sum()))

@@ -48,15 +48,15 @@ def test_store_of_every_page(dtype, dh, block, n_new):
 
 @pytest.mark.parametrize("dh", [64, 128, 192, 256])
 def test_uneven_queries_of_many_sequences(dh):
-    """Queries as they are in place of their planes, with two row waves: from the first tiles on, and from later ones."""
+    """One entry of the queries far above the others, and queries at the top of the range, with two row waves."""
     bounds.test_queries_with_one_entry_far_above_the_others(64, 8, 4, dh, 40, 130, 20)
     bounds.test_queries_with_one_entry_far_above_the_others(64, 8, 4, dh, 40, 130, 10)
     bounds.test_queries_at_the_top_of_the_range("bf16", 256, 128, dh, 40, 50)
 
 
-def test_planes_that_become_too_coarse_along_a_sequence():
-    """Keys 2^20 times larger from 2000 tokens on: the first blocks are within what planes of the queries may leave
-    out, later ones, in another batch of block numbers, are not."""
+def test_small_entries_that_count_late_in_a_sequence():
+    """Keys 2^20 times larger from 2000 tokens on: entries of the queries 2^-18 of the largest, in whose dim the keys
+    are 0, do nothing in the first blocks and decide in later ones, in another batch of block numbers."""
     import torch
     for hq, hkv, dh in ((2, 1, 128), (2, 1, 256)):
         T, length = 40, 2800

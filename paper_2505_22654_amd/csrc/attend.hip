@@ -60,6 +60,7 @@ constexpr int kWaves = kAttendWaves;
 constexpr float kNothing = -FLT_MAX;  // reference of a row that has seen no key: below every finite logit
 constexpr float kBias = 4.f;        // the largest weight is 2^4 when the reference is set ..
 constexpr float kRaise = 4096.f;    // .. and a lane's sum of a tile at most this until it is raised (fp16 holds 2^16)
+constexpr float kMostExp = 12.f;    // log2(kRaise)
 constexpr int kValueExp = -15;      // e4m3's 2^-9 times 2^-15 is fp16's smallest number
 constexpr int kWeightExp = -100;    // sums of weights without this factor stay inside fp32
 
@@ -128,6 +129,20 @@ __device__ __forceinline__ int exp_of(float s) {
     return min(max(e, kScaleExpMin), kScaleExpMax);
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+
+// References of large logits.  A reference is a rounded number, exponents are taken from exact products: from 2^25 on,
+// where numbers are 4 apart, the largest exponent may be other than kBias by as much, and by more than fp16 holds from
+// 2^28 on.  So a reference above its row's largest logit (`rest`: the largest exponent) goes down a step, and exponents
+// against a reference that has just been set are cut to kMostExp: keys within a step of the largest logit, which fp32
+// does not tell apart, then weigh the same.  (NaN stays NaN.)
+constexpr float kCoarse = 0x1p25f;
+__device__ __forceinline__ float lower_reference(float m, float now, float rest) {
+    if (!(fabsf(now) >= kCoarse && fabsf(now) < INFINITY) || !(rest < 0.f)) return now;
+    const int bits = __float_as_int(now);
+    return fmaxf(m, __int_as_float(now > 0.f ? bits - 1 : bits + 1));
+}
+template <bool kMost>
+__device__ __forceinline__ float at_most(float x) { return kMost && x > kMostExp ? kMostExp : x; }
 
 // Lengths of one sequence as the kernels use them.
 struct Span {
@@ -629,7 +644,8 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             if constexpr (kMask) v = at[0].there[u] && kt + u * kCacheGroup + 4 * g + r < row.lim ? v : -INFINITY;
             return v;
         };
-        auto weigh = [&](float ref) {
+        auto weigh = [&](float ref, auto most) {
+            constexpr bool kMost = decltype(most)::value;
             float all = 0.f;
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
@@ -637,7 +653,8 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                 sums[u] = 0.f;
 #pragma unroll
                 for (int r = 0; r < 4; r += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(logit(u, r, add)), p1 = __builtin_amdgcn_exp2f(logit(u, r + 1, add));
+                    const float p0 = __builtin_amdgcn_exp2f(at_most<kMost>(logit(u, r, add)));
+                    const float p1 = __builtin_amdgcn_exp2f(at_most<kMost>(logit(u, r + 1, add)));
                     typename O::pair pp[kP];
                     split<O, kP>(f32x2_t{p0, p1}, pp);
                     sums[u] += p0;
@@ -652,7 +669,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             }
             return all;
         };
-        if (__any(weigh(m) > kRaise) || sc.now > eref) {
+        if (__any(weigh(m, std::false_type()) > kRaise) || sc.now > eref) {
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kGroups; ++u)
@@ -660,13 +677,24 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
                 for (int r = 0; r < 4; ++r) top = fmaxf(top, logit(u, r, sc.weights[u]));
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
+            float now = fmaxf(m, top - kBias);
+            if (__builtin_expect(__any(fabsf(now) >= kCoarse && fabsf(now) < INFINITY), 0)) {
+                float rest = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) rest = fmaxf(rest, logit(u, r, sc.weights[u] - now));
+                rest = fmaxf(rest, __shfl_xor(rest, 16, kWave));
+                rest = fmaxf(rest, __shfl_xor(rest, 32, kWave));
+                now = lower_reference(m, now, rest);
+            }
+            const float f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
             m = now;
             eref = __builtin_amdgcn_readfirstlane(sc.now);
             l *= f;
 #pragma unroll
             for (int d = 0; d < kD; ++d) acc[d] *= fu;
-            weigh(now);
+            weigh(now, std::true_type());
         }
         if constexpr (kMask) {
 #pragma unroll
@@ -855,14 +883,16 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             if constexpr (kMask) v = at.there[r >> 3] && kt + 8 * (r >> 2) + 4 * g + (r & 3) < row.lim ? v : -INFINITY;
             return v;
         };
-        auto weigh = [&](float ref) {
+        auto weigh = [&](float ref, auto most) {
+            constexpr bool kMost = decltype(most)::value;
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) {
                 const float add = sc.weights[u] - ref;
                 sums[u] = 0.f;
 #pragma unroll
                 for (int r = 0; r < 8; r += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(logit(8 * u + r, add)), p1 = __builtin_amdgcn_exp2f(logit(8 * u + r + 1, add));
+                    const float p0 = __builtin_amdgcn_exp2f(at_most<kMost>(logit(8 * u + r, add)));
+                    const float p1 = __builtin_amdgcn_exp2f(at_most<kMost>(logit(8 * u + r + 1, add)));
                     typename O::pair pp[kP];
                     split<O, kP>(f32x2_t{p0, p1}, pp);
                     sums[u] += p0;
@@ -876,18 +906,26 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             }
             return sums[0] + sums[1];
         };
-        if (__any(weigh(m) > kRaise) || sc.now > eref) {
+        if (__any(weigh(m, std::false_type()) > kRaise) || sc.now > eref) {
             float top = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, logit(r, sc.weights[r >> 3]));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float now = fmaxf(m, top - kBias), f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
+            float now = fmaxf(m, top - kBias);
+            if (__builtin_expect(__any(fabsf(now) >= kCoarse && fabsf(now) < INFINITY), 0)) {
+                float rest = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) rest = fmaxf(rest, logit(r, sc.weights[r >> 3] - now));
+                rest = fmaxf(rest, __shfl_xor(rest, 32, kWave));
+                now = lower_reference(m, now, rest);
+            }
+            const float f = __builtin_amdgcn_exp2f(m - now), fu = f * pow2(eref - sc.now);
             m = now;
             eref = __builtin_amdgcn_readfirstlane(sc.now);
             l *= f;
 #pragma unroll
             for (int d = 0; d < kD; ++d) acc[d] *= fu;
-            weigh(now);
+            weigh(now, std::true_type());
         }
         if constexpr (kMask) {
 #pragma unroll

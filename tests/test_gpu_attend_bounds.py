@@ -213,3 +213,29 @@ def test_logits_with_a_large_product_keep_the_small_ones(hq, hkv, dh, T, length,
     want, bound = _many_rows_bound(shape, q, rows, cache, table, lens)
     over = (got.double() - want).abs() - bound - HALF_STEP["bf16"] * want.abs()
     assert float(over.max()) <= 0, (float(over.max()), int((over > 0).sum()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 3, 40])
+@pytest.mark.parametrize("size", [20, 28, 34, 60, 100])
+def test_large_logits_pick_a_key(dtype, T, size):
+    """Logits of 2^size and their half, where a step of fp32 is more than what an exponential holds from 2^31 on: the
+    key of the larger one has all weight, or its copies share it evenly."""
+    import torch
+    length = 333
+    shape = wl.CacheShape(dtype, 2, 4, 2, 64, 16, 44, 21, T, scale=1.0)
+    g = torch.Generator(device="cuda").manual_seed(size + T)
+    dt = vb._torch_dtype(dtype)
+    k = torch.rand((2, 2, length, 64), generator=g, device="cuda") * 0.4 + 0.1
+    q = torch.rand((2, 4, T, 64), generator=g, device="cuda") + 0.5
+    best = [0, 17, length - T]
+    k[:, :, best] = 1.3125                                               # one number, in e4m3 too
+    v = torch.randn((2, 2, length, 64), generator=g, device="cuda").to(dt)
+    lens = [length, length]
+    cache, table, rows = _stored(shape, k.to(dt), v, lens)
+    q = (q * 2.0 ** (size - 6)).to(dt)
+    got = vb.cache_attend(shape, q, cache, table, i32(lens))["out"].double()
+    picked = torch.stack([rows["v"][table.long()[:, j // 16], :, j % 16] for j in best]).double()
+    want = picked.mean(0).repeat_interleave(2, 1)[:, :, None].expand(-1, -1, T, -1)
+    bound = picked.abs().mean(0).repeat_interleave(2, 1)[:, :, None] * (2.0 ** -11 + 80 * 2.0 ** -24) + HALF_STEP[dtype] * want.abs()
+    assert bool(torch.isfinite(got).all()) and float(((got - want).abs() - bound).max()) <= 0

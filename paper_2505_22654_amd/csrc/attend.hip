@@ -10,7 +10,7 @@
 // memory), in one above, 2^-11 of each: a quarter of that is what is left in a sum of many keys, a tenth of the
 // result's own rounding, and the second plane's products would not hide (3 x 300 rows over 2604 keys 42 and 54 us,
 // 8 x 512 over 4096 167 and 220).  fp32 calls: q and the weights as three bf16 planes each, V as bf16.  (The 8-bit
-// instructions would take K as it is stored, with q in two planes, in 165 us where this takes 173.  But they drop what
+// instructions would take K as it is stored, with q in two planes, in 163 us where this takes 173.  But they drop what
 // lies 2^-11 to 2^-14 below the largest product of a sum, where those of bf16 keep 2^-21: logits with one large
 // product were off by 1e-2.)  K's scale goes into the logits; V's, a power of two, is taken
 // relative to the largest that the wave has met: down to 2^-15 with the values, beyond that with the weights, whose
@@ -29,13 +29,12 @@
 // second launch joins.
 //
 // Measured, bf16, dh = 128, GPU time of calls on one set of inputs: one token of 32 sequences with 32 heads, up to
-// 3427 keys, 127 us (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 44 us (53 on five sets
-// in turn); of one with 2304 keys 10.2 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096
-// keys 171 us (792 TFLOP/s of the two products; 164 to 178 on different cards), over 8192 314 us (875), over 16384
-// 605 us (914); 4 x 700 over 3000, 32 heads, 117 us (623); 3 x 300 over 2604, 28 of 4, 43 us (446: 396 workgroups on
-// 256 CUs).  Two planes and no maximum of a tile, against K in bf16 and one, in turn on one card: 165 and 177 us for
-// the first of these prompts, 300 and 328 for the second.  More rows a wave (64: 280 us where 32 took 179), eight
-// waves (245) and rows over all four waves (203) lost to this split.
+// 3427 keys, 127 us (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 45 us (53 on five sets
+// in turn); of one with 2304 keys 10.4 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096
+// keys 181 us (748 TFLOP/s of the two products; 173 on another card), over 8192 333 us (824), over 16384 643 us (860;
+// 616); 4 x 700 over 3000, 32 heads, 120 us (610; 115); 3 x 300 over 2604, 28 of 4, 46.5 us (413: 396 workgroups on
+// 256 CUs; 44).  With a maximum of every tile the first of these prompts took 4 us more.  More rows a wave (64: 280 us
+// where 32 took 179), eight waves (245) and rows over all four waves (203) lost to this split.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>

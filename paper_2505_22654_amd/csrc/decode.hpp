@@ -91,23 +91,23 @@ constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
 constexpr bool attend_many_fits(bool is_bf16, int head_dim) { return is_bf16 || head_dim <= 192; }
 // How a call is cut into workgroups: fills the last five fields from the others.
 // A workgroup of the few-row kernel holds one tile of 16 rows, of the many-row kernel 32 rows a wave.  16
-// sequences of 8 kv heads, 3000 keys, GPU time in us, few and many: 8 rows 19.8 and 21.5, 16 rows 20.3 and
-// 22.3, 20 rows (two tiles of 16) 24.2 and 21.8, 32 rows 26.6 and 22.7.  In fp32 with heads above 192 the many-row
+// sequences of 8 kv heads, 3000 keys, GPU time in us, few and many: 8 rows 20.1 and 20.8, 16 rows 20.5 and
+// 21.3, 20 rows (two tiles of 16) 24.4 and 21.0, 32 rows 26.8 and 22.0.  In fp32 with heads above 192 the many-row
 // kernel would not fit the registers (4 x 4 kv heads, 1024 rows, 2000 keys 208 us, few rows at a time 100; at
-// 192 65 and 79).
+// 192 66 and 81).
 // Two of the many-row kernel's waves share their keys, each with rows of its own, where that leaves a
 // workgroup a CU: keys are read half as often, but walked by half the waves.  One and two row waves, by
 // the workgroups that two make:
-//   1 x 4 kv heads, 63 rows, 2304 keys (4): 15.2, 19.5     4 x 4, 63 rows, 30000 keys (16): 30.6, 32.6
-//   16 x 8, 36 rows, 3000 keys (128): 25.1, 27.0           16 x 8, 64 rows (128): 28.2, 28.7
-//   64 x 4, 49 rows, 3000 keys (256): 46.6, 35.8           16 x 8, 192 rows (384): 72.7, 52.4
-//   64 x 8, 64 rows, 3000 keys (512): 89, 70               64 x 8, 80 rows (1024): 116, 122
+//   1 x 4 kv heads, 63 rows, 2304 keys (4): 14.1, 18.6     4 x 4, 63 rows, 30000 keys (16): 31.2, 33.9
+//   16 x 8, 36 rows, 3000 keys (128): 24.7, 27.7           16 x 8, 64 rows (128): 28.0, 29.2
+//   64 x 4, 49 rows, 3000 keys (256): 46.0, 37.6           16 x 8, 192 rows (384): 73.9, 54.8
+//   64 x 8, 64 rows, 3000 keys (512): 88, 70               64 x 8, 80 rows (1024): 113, 116
 // Keys are cut into chunks until every CU has one workgroup, as long as each wave has a tile of keys; more
 // chunks cost more in the joining launch than they bring:
-//   1 x 4 kv heads, 2304 keys: 1 chunk 15.4, 2 13.3, 3 11.3, 9 (a tile a wave) 10.3
-//   5 x 8 kv heads, 1391 keys in fp32: 1 chunk 14.4, 3 12.6, 6 11.3
-//   4 x 4 kv heads, up to 65536 keys: 8 chunks 52.7, 16 45.1, 32 46.4, 64 51.4, 128 64.7
-//   32 x 32 kv heads, up to 3427 keys: 1 chunk 128, 2 134, 4 144
+//   1 x 4 kv heads, 2304 keys: 1 chunk 15.4, 2 13.2, 3 11.4, 9 (a tile a wave) 10.3
+//   5 x 8 kv heads, 1391 keys in fp32: 1 chunk 14.5, 3 12.8, 6 11.5
+//   4 x 4 kv heads, up to 65536 keys: 8 chunks 52.9, 16 45.1, 32 46.6, 64 52.1, 128 65.2
+//   32 x 32 kv heads, up to 3427 keys: 1 chunk 129, 2 136, 4 146
 inline void attend_form(AttendArgs &a) {
     constexpr int64_t kCus = 256;
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T, heads = (int64_t)a.B * a.Hkv;

@@ -30,6 +30,8 @@ def test_plan_of_the_longest_rows(n_new):
     assert bool((held[:guard] == -7).all()) and bool((held[-guard:] == -7).all())
     for at in range(30, n_new, 1 << 28):
         assert bool((slots[0, at:at + (1 << 28)] == -1).all())
+    del held, slots, out
+    torch.cuda.empty_cache()
 
 
 def test_store_refuses_slabs_that_a_descriptor_does_not_hold():
@@ -44,3 +46,5 @@ def test_store_refuses_slabs_that_a_descriptor_does_not_hold():
     cache = vb.cache_alloc(shape)
     with pytest.raises(ValueError, match="rows"):
         vb.cache_store(shape, x, x, i32([[0, 1, 2]]), cache)
+    del far, x
+    torch.cuda.empty_cache()

@@ -135,8 +135,9 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 // against a reference that has just been set are cut to kMostExp: keys within a step of the largest logit, which fp32
 // does not tell apart, then weigh the same.  (NaN stays NaN.)
 constexpr float kCoarse = 0x1p25f;
+__device__ __forceinline__ bool is_coarse(float now) { return fabsf(now) >= kCoarse && fabsf(now) < FLT_MAX; }  // (kNothing is not)
 __device__ __forceinline__ float lower_reference(float m, float now, float rest) {
-    if (!(fabsf(now) >= kCoarse && fabsf(now) < INFINITY) || !(rest < 0.f)) return now;
+    if (!is_coarse(now) || !(rest < 0.f)) return now;
     const int bits = __float_as_int(now);
     return fmaxf(m, __int_as_float(now > 0.f ? bits - 1 : bits + 1));
 }
@@ -635,7 +636,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 
         Scales<kGroups, sizeof(T) == 2> sc;
         sc.of(at[0], eref);
-        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);  // (the products and the next keys' requests first)
         typename O::vec pb[kGroups / 2][kP];
         float sums[kGroups];
         auto logit = [&](int u, int r, float add) {
@@ -677,7 +678,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             float now = fmaxf(m, top - kBias);
-            if (__builtin_expect(__any(fabsf(now) >= kCoarse && fabsf(now) < INFINITY), 0)) {
+            if (__builtin_expect(__any(is_coarse(now)), 0)) {
                 float rest = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < kGroups; ++u)
@@ -874,7 +875,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
 
         Scales<kGroups, sizeof(T) == 2> sc;
         sc.of(at, eref);
-        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);  // (the products and the next keys' requests first)
         typename O::vec pb[kGroups][kP];
         float sums[kGroups];
         auto logit = [&](int r, float add) {
@@ -911,7 +912,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
             for (int r = 0; r < 16; ++r) top = fmaxf(top, logit(r, sc.weights[r >> 3]));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             float now = fmaxf(m, top - kBias);
-            if (__builtin_expect(__any(fabsf(now) >= kCoarse && fabsf(now) < INFINITY), 0)) {
+            if (__builtin_expect(__any(is_coarse(now)), 0)) {
                 float rest = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) rest = fmaxf(rest, logit(r, sc.weights[r >> 3] - now));

@@ -5,16 +5,15 @@
 // takes them, so they never leave the registers.  The cache is stored in operand order: a lane's 16
 // bytes are one load, and nothing is staged in LDS.
 //
-// bf16 calls: K (as bf16, exact) times q; V as fp16 (exact) times the weights in fp16: in two planes for up to 16
-// rows, whose sum is a weight to 2^-22 (32 sequences of up to 3427 keys 126.1 us with one, 127.8 with two, bound by
-// memory), in one above, 2^-11 of each: a quarter of that is what is left in a sum of many keys, a tenth of the
-// result's own rounding, and the second plane's products would not hide (3 x 300 rows over 2604 keys 42 and 54 us,
-// 8 x 512 over 4096 167 and 220).  fp32 calls: q and the weights as three bf16 planes each, V as bf16.  (The 8-bit
-// instructions would take K as it is stored, with q in two planes, in 163 us where this takes 173.  But they drop what
-// lies 2^-11 to 2^-14 below the largest product of a sum, where those of bf16 keep 2^-21: logits with one large
-// product were off by 1e-2.)  K's scale goes into the logits; V's, a power of two, is taken
-// relative to the largest that the wave has met: down to 2^-15 with the values, beyond that with the weights, whose
-// reference it then enters, so that the largest contributions keep their bits.
+// bf16 calls: K (as bf16, exact) times q; V as fp16 (exact) times the weights as two fp16 planes, whose sum is a
+// weight to 2^-22.  (With one, 2^-11 of each weight, a sum of many keys is off by a tenth of the result's own
+// rounding, and 7 % of the results are another bf16 number.  That takes 180 us where two planes take 232, 512 rows of 8
+// sequences over 4096 keys; 46 and 56, 3 x 300 over 2604; 126 and 128, one of 32 sequences, bound by memory.)  fp32
+// calls: q and the weights as three bf16 planes each, V as bf16.  (The 8-bit instructions would take K as it is
+// stored, with q in two planes, 6 % faster.  But they drop what lies 2^-11 to 2^-14 below the largest product of a
+// sum, where those of bf16 keep 2^-21: logits with one large product were off by 1e-2.)  K's scale goes into the
+// logits; V's, a power of two, is taken relative to the largest that the wave has met: down to 2^-15 with the values,
+// beyond that with the weights, whose reference it then enters, so that the largest contributions keep their bits.
 // Softmax in one pass against a reference that is raised only where a lane's weights of a tile add up to more
 // than 2^12, so that most tiles need no exchange between lanes and no maximum.
 //
@@ -31,10 +30,10 @@
 // Measured, bf16, dh = 128, GPU time of calls on one set of inputs: one token of 32 sequences with 32 heads, up to
 // 3427 keys, 127 us (5.4 TB/s from memory); of 4 sequences with 28 heads of 4, up to 65536 keys, 45 us (53 on five sets
 // in turn); of one with 2304 keys 10.4 us, two launches' latency.  512 tokens of 8 sequences, 28 heads of 4, over 4096
-// keys 181 us (748 TFLOP/s of the two products; 173 on another card), over 8192 333 us (824), over 16384 643 us (860;
-// 616); 4 x 700 over 3000, 32 heads, 120 us (610; 115); 3 x 300 over 2604, 28 of 4, 46.5 us (413: 396 workgroups on
-// 256 CUs; 44).  With a maximum of every tile the first of these prompts took 4 us more.  More rows a wave (64: 280 us
-// where 32 took 179), eight waves (245) and rows over all four waves (203) lost to this split.
+// keys 230 us (589 TFLOP/s of the two products), over 8192 440 us (624), over 16384 854 us (648); 4 x 700 over 3000, 32
+// heads, 145 us (505); 3 x 300 over 2604, 28 of 4, 56 us (343: 396 workgroups on 256 CUs).  With one plane of the
+// weights a maximum of every tile took 4 us more in the first of these prompts, and more rows a wave (64: 280 us where
+// 32 took 179), eight waves (245) and rows over all four waves (203) lost to this split.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -69,7 +68,7 @@ template <>
 struct Operand<bf16_t> {
     typedef f16x8_t vec;
     typedef f16x2_t pair;
-    static constexpr int kFewPlanes = 2, kManyPlanes = 1, kQueryPlanes = 1;
+    static constexpr int kPlanes = 2, kQueryPlanes = 1;
     static __device__ __forceinline__ pair from_fp8(uint32_t w, float s, bool hi) {
         return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, false);
     }
@@ -84,7 +83,7 @@ template <>
 struct Operand<float> {
     typedef bf16x8_t vec;
     typedef bf16x2_t pair;
-    static constexpr int kFewPlanes = 3, kManyPlanes = 3, kQueryPlanes = 3;
+    static constexpr int kPlanes = 3, kQueryPlanes = 3;
     static __device__ __forceinline__ pair from_fp8(uint32_t w, float s, bool hi) {
         return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
     }
@@ -570,7 +569,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     constexpr int kTile = attend_tile(1), kGroups = kTile / kCacheGroup;
     constexpr int kH = DP / 64;  // 16-byte loads per lane and group
     constexpr int kD = DP / 16;  // tiles of 16 dims
-    constexpr int kQ = O::kQueryPlanes, kP = O::kFewPlanes, step = kTile * kWaves;
+    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes, step = kTile * kWaves;
     extern __shared__ float4 lds4[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -787,7 +786,7 @@ __global__ __launch_bounds__(kWaves *kWave, DP <= 128 && sizeof(T) == 2 ? 2 : 1)
     constexpr bool kOdd = DP % 128 != 0;        // and a last 64 dims: half a piece
     constexpr int kD = DP / 32;                 // tiles of 32 dims
     constexpr int kKeyWaves = kWaves / kRowWaves;  // waves that share rows
-    constexpr int kQ = O::kQueryPlanes, kP = O::kManyPlanes, step = kTile * kKeyWaves;
+    constexpr int kQ = O::kQueryPlanes, kP = O::kPlanes, step = kTile * kKeyWaves;
     extern __shared__ float4 lds4[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave % kKeyWaves, row_wave = wave / kKeyWaves;

@@ -91,17 +91,19 @@ constexpr int attend_tile(int row_tiles) { return row_tiles > 1 ? 32 : 64; }
 constexpr bool attend_many_fits(bool is_bf16, int head_dim) { return is_bf16 || head_dim <= 192; }
 // How a call is cut into workgroups: fills the last five fields from the others.
 // A workgroup of the few-row kernel holds one tile of 16 rows, of the many-row kernel 32 rows a wave.  16
-// sequences of 8 kv heads, 3000 keys, GPU time in us, few and many: 8 rows 20.1 and 20.8, 16 rows 20.5 and
-// 21.3, 20 rows (two tiles of 16) 24.4 and 21.0, 32 rows 26.8 and 22.0.  In fp32 with heads above 192 the many-row
+// sequences of 8 kv heads, 3000 keys, GPU time in us, few and many: 8 rows 19.9 and 21.6, 16 rows 20.4 and
+// 22.3, 20 rows (two tiles of 16) 24.5 and 22.3, 32 rows 26.7 and 23.1.  In fp32 with heads above 192 the many-row
 // kernel would not fit the registers (4 x 4 kv heads, 1024 rows, 2000 keys 208 us, few rows at a time 100; at
-// 192 66 and 81).
+// 192 66 and 82).
 // Two of the many-row kernel's waves share their keys, each with rows of its own, where that leaves a
-// workgroup a CU: keys are read half as often, but walked by half the waves.  One and two row waves, by
-// the workgroups that two make:
-//   1 x 4 kv heads, 63 rows, 2304 keys (4): 14.1, 18.6     4 x 4, 63 rows, 30000 keys (16): 31.2, 33.9
-//   16 x 8, 36 rows, 3000 keys (128): 24.7, 27.7           16 x 8, 64 rows (128): 28.0, 29.2
-//   64 x 4, 49 rows, 3000 keys (256): 46.0, 37.6           16 x 8, 192 rows (384): 73.9, 54.8
-//   64 x 8, 64 rows, 3000 keys (512): 88, 70               64 x 8, 80 rows (1024): 113, 116
+// workgroup a CU: keys are read half as often, but walked by half the waves; not for three tiles of 32 rows, which
+// two waves would take as four.  One and two row waves, by the workgroups that two make:
+//   1 x 4 kv heads, 63 rows, 2304 keys (4): 14.2, 18.8     4 x 4, 63 rows, 30000 keys (16): 36.2, 39.0
+//   16 x 8, 36 rows, 3000 keys (128): 27.7, 31.8           16 x 8, 64 rows (128): 29.3, 33.0
+//   64 x 4, 49 rows, 3000 keys (256): 48.1, 44.9           16 x 8, 192 rows (384): 75.6, 68.0
+//   64 x 8, 64 rows, 3000 keys (512): 92, 80               64 x 8, 128 rows (1024): 155, 133
+//   three tiles: 64 x 8, 80 rows (1024): 118, 137; 96 rows 124, 133; 64 x 4, 96 rows, 2000 keys, heads of 256 99, 111
+// (Of an odd number of tiles above that it is either: 64 x 8, 160 rows 188, 173, 224 rows 241, 257, 288 rows 300, 276.)
 // Keys are cut into chunks until every CU has one workgroup, as long as each wave has a tile of keys; more
 // chunks cost more in the joining launch than they bring:
 //   1 x 4 kv heads, 2304 keys: 1 chunk 15.4, 2 13.2, 3 11.4, 9 (a tile a wave) 10.3
@@ -111,9 +113,10 @@ constexpr bool attend_many_fits(bool is_bf16, int head_dim) { return is_bf16 || 
 inline void attend_form(AttendArgs &a) {
     constexpr int64_t kCus = 256;
     const int64_t rows = (int64_t)(a.Hq / a.Hkv) * a.T, heads = (int64_t)a.B * a.Hkv;
-    const int64_t pair = 4 * kCacheGroup;  // rows of two row waves
     a.row_tiles = rows <= kCacheGroup || !attend_many_fits(a.is_bf16, a.dh) ? 1 : 2;
-    a.row_waves = a.row_tiles == 2 && rows > 2 * kCacheGroup && heads * ((rows + pair - 1) / pair) >= kCus ? 2 : 1;
+    const int64_t tiles = (rows + 2 * kCacheGroup - 1) / (2 * kCacheGroup);  // of a row wave
+    const bool three = tiles == 3 && heads * tiles < (int64_t)1 << 24;  // (as one grid takes them)
+    a.row_waves = a.row_tiles == 2 && tiles > 1 && !three && heads * ((tiles + 1) / 2) >= kCus ? 2 : 1;
     const int block = kCacheGroup * a.row_tiles * a.row_waves;
     a.row_blocks = (int)((rows + block - 1) / block);
     const int64_t units = heads * a.row_blocks;

@@ -49,9 +49,9 @@ def test_store_of_every_page(dtype, dh, block, n_new):
 @pytest.mark.parametrize("dh", [64, 128, 192, 256])
 def test_uneven_queries_of_many_sequences(dh):
     """One entry of the queries far above the others, and queries at the top of the range, with two row waves."""
-    bounds.test_queries_with_one_entry_far_above_the_others(64, 8, 4, dh, 40, 130, 20)
-    bounds.test_queries_with_one_entry_far_above_the_others(64, 8, 4, dh, 40, 130, 10)
-    bounds.test_queries_at_the_top_of_the_range("bf16", 256, 128, dh, 40, 50)
+    bounds.test_queries_with_one_entry_far_above_the_others(64, 8, 4, dh, 50, 130, 20)
+    bounds.test_queries_with_one_entry_far_above_the_others(64, 8, 4, dh, 50, 130, 10)
+    bounds.test_queries_at_the_top_of_the_range("bf16", 256, 128, dh, 50, 50)
 
 
 def test_small_entries_that_count_late_in_a_sequence():
@@ -71,6 +71,6 @@ def test_small_entries_that_count_late_in_a_sequence():
         q[..., 7] = 2.0 ** 7
         q = q.bfloat16()
         got = vb.cache_attend(shape, q, cache, table, _i32([length]))["out"]
-        want, bound = bounds._many_rows_bound(shape, q, rows, cache, table, [length])
+        want, bound = bounds._two_planes_bound(shape, q, rows, cache, table, [length])
         over = (got.double() - want).abs() - bound - 2.0 ** -8 * want.abs()
         assert float(over.max()) <= 0, (dh, float(over.max()))
